@@ -204,6 +204,101 @@ int escoin_sconv_forward_tiled(const escoin_conv_desc *desc, const void *plan_ho
 int escoin_sconv_tiled_on_matrix_cores(const escoin_conv_desc *desc, const void *plan_host);
 int escoin_sconv_tiled_kernel(const escoin_conv_desc *desc, const void *plan_host);
 
+/* ---------------------------------------------------------------------------------------
+ * Pruned feed-forward blocks: linear layers on token-major activations, and the norms between them.
+ *
+ * Conventions beside those at the top of this file
+ *   - Activations are T x features, one row a token, features contiguous; rows may lie further apart (ld_*, in
+ *     elements; 0: next to each other).  Every tensor of a call, parameters too, has the descriptor's type; pointers are
+ *     aligned to it.  Sums and statistics are fp32, an output is rounded once (to nearest even).
+ *   - T == 0 is a call that does nothing and returns ESCOIN_OK.  Rows from T on are neither read nor written.
+ */
+enum { ESCOIN_T_F32 = 0, ESCOIN_T_F16 = 1, ESCOIN_T_BF16 = 2 };
+
+enum {
+    /* ESCOIN_F_BIAS and ESCOIN_F_RELU as above, and: */
+    ESCOIN_F_RESIDUAL = 4u,   /* add residual[t][m] to the result                               */
+    ESCOIN_F_SILU = 8u,       /* z / (1 + exp(-z))                                              */
+    ESCOIN_F_GELU = 16u,      /* z/2 * erfc(-z / sqrt(2))                                       */
+    ESCOIN_F_GELU_TANH = 32u  /* z/2 * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3)))              */
+};
+
+typedef struct escoin_linear_desc {
+    int32_t T, K, M; /* tokens, input features, output features                             */
+    int32_t type;    /* ESCOIN_T_*                                                          */
+    int32_t gated;   /* 0, or 1: act(gate) * up, from a CSR of 2*M rows, the gates' first   */
+    int64_t ld_in, ld_out, ld_residual; /* elements from row to row; 0: K, M, M             */
+} escoin_linear_desc;
+
+/* Validates a descriptor: ESCOIN_EINVAL for T < 0, K or M < 1, an unknown type or a row pitch shorter than its row,
+ * ESCOIN_ERANGE where 2*M or K reaches 2^30 or a pitch 2^40. */
+int escoin_linear_check_desc(const escoin_linear_desc *desc);
+
+/*
+ * Pruned linear layer.  With W (M x K, or 2*M x K gated) given by its nonzeros as CSR,
+ *   out[t][m] = act(sum_k W[m][k] * in[t][k] + bias[m]) + residual[t][m]
+ *   gated:      act(sum_k W[m][k] * in[t][k] + bias[m]) * (sum_k W[M+m][k] * in[t][k] + bias[M+m]) + residual[t][m]
+ * The plan (host blob, then uploaded, as for the convolution) holds the weights rounded to the descriptor's type
+ * (beyond its range: infinite), each with a bit for its place, in the order in which the matrix cores take them; plans for
+ * more tokens than escoin_linear_few_tokens tells hold them a second time with their zeros.  `T` of the descriptor that a plan is
+ * built with is the most tokens that calls with it may have.
+ *   rowptr, colidx, value  host CSR, columns of a row in any order; repeated ones are added up in fp32
+ *   plan_size     an upper bound on the blob's size, from the descriptor and the number of nonzeros
+ *   plan_build    fills it; ESCOIN_ESIZE if it is smaller than plan_size tells, ESCOIN_EINVAL on a malformed CSR
+ * Both run on the host and need no GPU.
+ */
+int escoin_linear_plan_size(const escoin_linear_desc *desc, const int32_t *rowptr, const int32_t *colidx, size_t *plan_bytes);
+int escoin_linear_plan_build(const escoin_linear_desc *desc, const int32_t *rowptr, const int32_t *colidx,
+                             const float *value, void *plan, size_t plan_bytes);
+
+/*
+ * One forward call.  Up to escoin_linear_few_tokens tokens a kernel reads each kept weight once and multiplies it on the
+ * matrix cores as it comes, beyond that the weights are multiplied in tiles, zeros too.  Pruned weights count as zeros: an Inf
+ * or NaN in a token's input makes every output of that token NaN (or what the epilogue makes of it), and of no other token.
+ * The order of the sums depends on T, never on timing: equal calls give equal bits.
+ *   plan_host     host pointer to the blob (its header is read at the call), d_plan its copy on the device, 16-byte aligned
+ *   d_bias        device, M (gated: 2*M) elements, with ESCOIN_F_BIAS
+ *   d_residual    device, with ESCOIN_F_RESIDUAL; may be d_out itself with the same pitch (each element is read before it is
+ *                 written), and must not overlap it otherwise
+ *   flags         ESCOIN_F_BIAS, ESCOIN_F_RESIDUAL and at most one activation
+ * Inputs whose rows start on 16-byte boundaries, and hold a multiple of 16 bytes, are read with wide loads; any other is accepted.
+ */
+int escoin_linear_forward(const escoin_linear_desc *desc, const void *plan_host, const void *d_plan, const void *d_in,
+                          void *d_out, const void *d_bias, const void *d_residual, uint32_t flags, void *hip_stream);
+/* host: up to how many tokens a call with this plan reads the kept weights only; or an error code */
+int escoin_linear_few_tokens(const escoin_linear_desc *desc, const void *plan_host);
+
+enum { ESCOIN_NORM_NONE = 0, ESCOIN_NORM_RMS = 1, ESCOIN_NORM_LAYER = 2 };
+
+typedef struct escoin_norm_desc {
+    int32_t T, D;        /* tokens, features                                                    */
+    int32_t type;        /* ESCOIN_T_*                                                          */
+    int32_t post, pre;   /* ESCOIN_NORM_*: of the block's output y, and of the sum h            */
+    int32_t gate_rows;   /* 0: one gate vector for all tokens; 1: a row for each token          */
+    float eps;           /* added to the mean square (or variance), >= 0                        */
+    float alpha, beta;   /* scales of the residual stream and of the block's output             */
+    float weight_offset; /* added to every norm weight (1 where weights are kept as w - 1)      */
+    int64_t ld_x, ld_y, ld_gate, ld_h, ld_n; /* elements from row to row; 0: D                  */
+} escoin_norm_desc;
+
+int escoin_norm_check_desc(const escoin_norm_desc *desc);
+
+/*
+ * The residual stream between two blocks, in one pass over it:
+ *   h[t] = alpha * x[t] + beta * gate * post(y[t])       n[t] = pre(h[t])
+ *   RMS(v) = v / sqrt(mean(v^2) + eps) * (weight + weight_offset) + bias
+ *   LAYER(v): of v - mean(v), with the variance in place of the mean square;   NONE(v) = v
+ * n is the norm of h before h is rounded.
+ *   d_x                  device, T x D
+ *   d_y, d_gate          device; d_y NULL: h = alpha * x (post must be NONE then, and d_gate NULL); d_gate NULL: 1
+ *   d_post_*, d_pre_*    device, D elements each; NULL: weight 1, bias 0; NULL for a norm that is NONE
+ *   d_h, d_n             device, T x D each; either may be NULL.  Each may be d_x or d_y itself with the same pitch; h and n
+ *                        must not be the same.
+ */
+int escoin_norm_forward(const escoin_norm_desc *desc, const void *d_x, const void *d_y, const void *d_gate,
+                        const void *d_post_weight, const void *d_post_bias, const void *d_pre_weight, const void *d_pre_bias,
+                        void *d_h, void *d_n, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -16,6 +16,9 @@ LIB_PATH = os.path.join(_HERE, "libescoin.so")
 
 OK, EINVAL, ERANGE, EHIP, ESIZE = 0, -1, -2, -3, -4
 F_BIAS, F_RELU = 1, 2
+F_RESIDUAL, F_SILU, F_GELU, F_GELU_TANH = 4, 8, 16, 32
+T_F32, T_F16, T_BF16 = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 
 
 class escoin_conv_desc(ctypes.Structure):
@@ -24,6 +27,17 @@ class escoin_conv_desc(ctypes.Structure):
 
 class escoin_sconv_tuning(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int32) for k in ("K", "Q", "B", "WM", "CC", "NB", "TH", "CS", "WS", "CC0")]
+
+
+class escoin_linear_desc(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int32) for k in ("T", "K", "M", "type", "gated")]
+                + [(k, ctypes.c_int64) for k in ("ld_in", "ld_out", "ld_residual")])
+
+
+class escoin_norm_desc(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int32) for k in ("T", "D", "type", "post", "pre", "gate_rows")]
+                + [(k, ctypes.c_float) for k in ("eps", "alpha", "beta", "weight_offset")]
+                + [(k, ctypes.c_int64) for k in ("ld_x", "ld_y", "ld_gate", "ld_h", "ld_n")])
 
 
 class EscoinError(RuntimeError):
@@ -63,6 +77,14 @@ def lib() -> ctypes.CDLL:
         L.escoin_sconv_forward_tiled.argtypes = [D, vp, vp, vp, vp, vp, ctypes.c_uint32, vp]
         L.escoin_sconv_tiled_on_matrix_cores.argtypes = [D, vp]
         L.escoin_sconv_tiled_kernel.argtypes = [D, vp]
+        LD, ND = ctypes.POINTER(escoin_linear_desc), ctypes.POINTER(escoin_norm_desc)
+        L.escoin_linear_check_desc.argtypes = [LD]
+        L.escoin_linear_plan_size.argtypes = [LD, vp, vp, ctypes.POINTER(ctypes.c_size_t)]
+        L.escoin_linear_plan_build.argtypes = [LD, vp, vp, vp, vp, ctypes.c_size_t]
+        L.escoin_linear_forward.argtypes = [LD, vp, vp, vp, vp, vp, vp, ctypes.c_uint32, vp]
+        L.escoin_linear_few_tokens.argtypes = [LD, vp]
+        L.escoin_norm_check_desc.argtypes = [ND]
+        L.escoin_norm_forward.argtypes = [ND, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -213,6 +235,147 @@ def escoin_sconv_tiled_kernel(desc, plan_host: np.ndarray) -> int:
     if rc < 0:
         _check(rc, "escoin_sconv_tiled_kernel")
     return rc
+
+
+def make_linear_desc(T, K, M, type, gated=False, ld_in=0, ld_out=0, ld_residual=0) -> escoin_linear_desc:
+    """T tokens (for a plan: the most a call may have), K input and M output features, type T_F32, T_F16 or T_BF16."""
+    return escoin_linear_desc(T, K, M, type, int(gated), ld_in, ld_out, ld_residual)
+
+
+def make_norm_desc(T, D, type, post=NORM_NONE, pre=NORM_RMS, gate_rows=0, eps=1e-5, alpha=1.0, beta=1.0, weight_offset=0.0,
+                   ld_x=0, ld_y=0, ld_gate=0, ld_h=0, ld_n=0) -> escoin_norm_desc:
+    return escoin_norm_desc(T, D, type, post, pre, gate_rows, eps, alpha, beta, weight_offset, ld_x, ld_y, ld_gate, ld_h, ld_n)
+
+
+def _torch_type(type):
+    import torch
+    return (torch.float32, torch.float16, torch.bfloat16)[type]
+
+
+class _Rows:
+    """Checks the device tensors of one call: all on one device, of one type; rows of contiguous elements, or vectors."""
+
+    def __init__(self, type):
+        self.type, self.device = _torch_type(type), None
+
+    def _seen(self, t):
+        if not t.is_cuda:
+            raise TypeError("device arguments must be CUDA tensors")
+        if t.dtype != self.type:
+            raise TypeError(f"device tensor has dtype {t.dtype}, expected {self.type}")
+        if self.device is None:
+            self.device = t.device
+        elif t.device != self.device:
+            raise TypeError(f"tensors of one call lie on {self.device} and on {t.device}")
+
+    def rows(self, t, T, width, ld):
+        """Pointer to T rows of `width` elements, `ld` (0: width) apart, or None."""
+        if t is None:
+            return None
+        self._seen(t)
+        if t.dim() != 2 or t.shape[0] < T or t.shape[1] != width or (width > 1 and t.stride(1) != 1) or (T > 1 and t.stride(0) != (ld or width)):
+            raise TypeError(f"expected {T} rows of {width}, {ld or width} elements apart: got shape {tuple(t.shape)}, strides {t.stride()}")
+        return t.data_ptr()
+
+    def vector(self, t, width):
+        if t is None:
+            return None
+        self._seen(t)
+        if t.numel() != width or not t.is_contiguous():
+            raise TypeError(f"expected {width} contiguous elements: got shape {tuple(t.shape)}, strides {t.stride()}")
+        return t.data_ptr()
+
+    def call(self, where, fn, *args, stream):
+        """The library launches on the current device: the tensors' own for the time of the call."""
+        import torch
+        if self.device.index != torch.cuda.current_device():
+            with torch.cuda.device(self.device):
+                return _check(fn(*args, _stream(stream)), where)
+        _check(fn(*args, _stream(stream)), where)
+
+
+def escoin_linear_check_desc(desc) -> int:
+    return lib().escoin_linear_check_desc(ctypes.byref(desc))
+
+
+def _csr(desc, rowptr, colidx, value=None):
+    """The arrays' pointers, once they are as long as they say (the library cannot tell)."""
+    p = _hptr(rowptr, np.int32), _hptr(colidx, np.int32), _hptr(value, np.float32)
+    rows = desc.M * (2 if desc.gated else 1)
+    if rowptr is not None:
+        if rowptr.size != rows + 1:
+            raise TypeError(f"rowptr has {rowptr.size} entries, expected {rows + 1}")
+        for a in (colidx, value):
+            if a is not None and a.size < rowptr[-1]:
+                raise TypeError(f"an array of {a.size} elements for {rowptr[-1]} nonzeros")
+    return p
+
+
+def escoin_linear_plan_size(desc, rowptr: np.ndarray, colidx: np.ndarray) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().escoin_linear_plan_size(ctypes.byref(desc), *_csr(desc, rowptr, colidx)[:2], ctypes.byref(n)), "escoin_linear_plan_size")
+    return n.value
+
+
+def escoin_linear_plan_build(desc, rowptr: np.ndarray, colidx: np.ndarray, value: np.ndarray, plan: np.ndarray | None = None) -> np.ndarray:
+    """Returns the plan blob as a uint8 numpy array (host)."""
+    if plan is None:
+        plan = np.empty(escoin_linear_plan_size(desc, rowptr, colidx), dtype=np.uint8)
+    _check(lib().escoin_linear_plan_build(ctypes.byref(desc), *_csr(desc, rowptr, colidx, value), _hptr(plan, np.uint8), plan.nbytes),
+           "escoin_linear_plan_build")
+    return plan
+
+
+def escoin_linear_few_tokens(desc, plan_host: np.ndarray) -> int:
+    rc = lib().escoin_linear_few_tokens(ctypes.byref(desc), _plan_ptr(plan_host))
+    if rc < 0:
+        _check(rc, "escoin_linear_few_tokens")
+    return rc
+
+
+class _LinearHeader(ctypes.Structure):
+    """Mirror of the linear plan's header (csrc/linear.h), for diagnostics and tests."""
+    _fields_ = ([(k, ctypes.c_uint32) for k in ("magic", "version")]
+                + [(k, ctypes.c_int32) for k in ("K", "M", "type", "gated", "most_tokens", "few_tokens", "most_tile_bytes", "reserved")]
+                + [(k, ctypes.c_uint64) for k in ("off_zero", "off_mask", "off_start", "off_kept", "off_whole", "total_bytes")])
+
+
+def _plan_ptr(plan: np.ndarray):
+    if plan is not None and plan.nbytes < ctypes.sizeof(_LinearHeader):
+        raise TypeError("this is no plan of a linear layer")
+    return _hptr(plan, np.uint8)
+
+
+def linear_plan_header(plan: np.ndarray) -> dict:
+    """Decodes the (opaque) header of a linear layer's plan."""
+    h = _LinearHeader.from_buffer_copy(plan[:ctypes.sizeof(_LinearHeader)].tobytes())
+    return {k: int(getattr(h, k)) for k, _ in _LinearHeader._fields_}
+
+
+def escoin_linear_forward(desc, plan_host: np.ndarray, d_plan, d_in, d_out, d_bias=None, d_residual=None, flags=0, stream=None):
+    t = _Rows(desc.type)
+    T, rows = max(desc.T, 0), desc.M * (2 if desc.gated else 1)
+    args = (t.rows(d_in, T, desc.K, desc.ld_in), t.rows(d_out, T, desc.M, desc.ld_out), t.vector(d_bias, rows),
+            t.rows(d_residual, T, desc.M, desc.ld_residual))
+    if d_plan.device != t.device or d_plan.nbytes < plan_host.nbytes:
+        raise TypeError("the plan's copy has to be whole and on the tensors' device")
+    t.call("escoin_linear_forward", lib().escoin_linear_forward, ctypes.byref(desc), _plan_ptr(plan_host), d_plan.data_ptr(), *args, flags,
+           stream=stream)
+
+
+def escoin_norm_check_desc(desc) -> int:
+    return lib().escoin_norm_check_desc(ctypes.byref(desc))
+
+
+def escoin_norm_forward(desc, d_x, d_h, d_n, d_y=None, d_gate=None, d_post_weight=None, d_post_bias=None, d_pre_weight=None,
+                        d_pre_bias=None, stream=None):
+    """`d_h` or `d_n` may be None: that output is not wanted."""
+    t = _Rows(desc.type)
+    T, D = max(desc.T, 0), desc.D
+    gate = t.rows(d_gate, T, D, desc.ld_gate) if desc.gate_rows else t.vector(d_gate, D)
+    x, y, h, n = (t.rows(v, T, D, ld) for v, ld in ((d_x, desc.ld_x), (d_y, desc.ld_y), (d_h, desc.ld_h), (d_n, desc.ld_n)))
+    params = [t.vector(v, D) for v in (d_post_weight, d_post_bias, d_pre_weight, d_pre_bias)]
+    t.call("escoin_norm_forward", lib().escoin_norm_forward, ctypes.byref(desc), x, y, gate, *params, h, n, stream=stream)
 
 
 class _PlanHeader(ctypes.Structure):
