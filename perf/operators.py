@@ -155,12 +155,12 @@ def _plan(w, T, M, type, gated):
     return dict(desc=desc, plan=plan, d_plan=torch.from_numpy(plan).cuda())
 
 
-def _norm_desc(T, D, type, post, pre):
+def _norm_desc(T, D, type, post, pre, gate="vector"):
     import paper_1802_10280_amd as esc
 
     kinds = {"none": esc.NORM_NONE, "rms": esc.NORM_RMS, "layer": esc.NORM_LAYER}
     return esc.make_norm_desc(T, D, {"f32": esc.T_F32, "f16": esc.T_F16, "bf16": esc.T_BF16}[type], kinds[post], kinds[pre],
-                              eps=EPS, alpha=ALPHA, beta=BETA)
+                              gate_rows=int(gate == "token"), eps=EPS, alpha=ALPHA, beta=BETA)
 
 
 def prepare(case, seed):
@@ -178,7 +178,7 @@ def prepare(case, seed):
         s["layer"] = _plan(s.pop("w"), T, case["M"], case["type"], case["gated"])
         s["out"] = new(T, case["M"])
     elif case["op"] == "norm":
-        s["desc"] = _norm_desc(T, case["D"], case["type"], case["post"] if case["y"] else "none", case["pre"])
+        s["desc"] = _norm_desc(T, case["D"], case["type"], case["post"] if case["y"] else "none", case["pre"], case["gate"])
         s["h"] = new(T, case["D"]) if case["y"] else None
         s["n"] = new(T, case["D"]) if case["pre"] != "none" else None
     else:
