@@ -112,13 +112,16 @@ __device__ inline u4 input16(const LinearArgs& a, const char* row, int at, int e
     } else {
         typedef typename Num<TYPE>::type N;
         constexpr int kN = 16 / sizeof(N);
+        struct __attribute__((packed, aligned(sizeof(N)))) Raw {
+            u4 v;
+        };
+        if (at + 16 <= end) return ((const Raw*)(row + at))->v;
         typedef N Nv __attribute__((ext_vector_type(kN)));
-        Nv v;
+        Nv v = {};
+        if (at < end)
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            const int b = at + i * (int)sizeof(N);
-            v[i] = *(const N*)(b < end ? row + b : a.zero);
-        }
+            for (int i = 0; i < kN; ++i)
+                if (at + i * (int)sizeof(N) < end) v[i] = ((const N*)(row + at))[i];
         return __builtin_bit_cast(u4, v);
     }
 }

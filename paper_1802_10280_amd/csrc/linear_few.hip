@@ -7,6 +7,9 @@ namespace {
 
 constexpr int kMostWaves = 16;
 
+// LDS of a wave: a tile's values; a lane reads up to 12 bytes from where its own end
+constexpr int few_buffer(int chunks) { return chunks * 1024 + 16; }
+
 // Exclusive sums over the lanes of a wave.
 __device__ inline int lanes_before(int n) {
     int s = n;
@@ -21,25 +24,12 @@ __device__ inline int lanes_before(int n) {
     return s - n;
 }
 
-// A tile on its way: its mask and the 16 bytes a lane carries of every 1024 of its values.
-template <int CHUNKS>
+// A tile on its way: its mask, the 16 bytes a lane carries of every 1024 of its values, and (AHEAD) its inputs.
+template <int CHUNKS, int PIECES>
 struct Load {
-    u4 v[CHUNKS];
+    u4 v[CHUNKS], x[PIECES];
     uint32_t mask;
 };
-
-template <int CHUNKS>
-__device__ inline void ask(const LinearArgs& a, int64_t tile, int lane, Load<CHUNKS>& l) {
-    const uint32_t begin = a.start[tile], end = a.start[tile + 1];
-    const int bytes = (int)(end - begin) * 16;
-    const char* const from = a.kept + (uint64_t)begin * 16;
-    l.mask = a.mask[tile * 64 + lane];
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-        const int at = c * 1024 + lane * 16;
-        l.v[c] = *(const u4*)(at < bytes ? from + at : a.zero);
-    }
-}
 
 // The eight weights of block b, zeros in their places, for a lane whose values start `at` bytes into LDS.
 template <int TYPE>
@@ -58,12 +48,11 @@ __device__ inline void expand(const char* values, const u2* picks, uint32_t mask
         for (int n = 0; n < 2; ++n) {
             const uint32_t nibble = mask >> (8 * b + 4 * n) & 15;
             const u2 pick = picks[nibble];
-            struct __attribute__((packed, aligned(2))) Near {
-                uint32_t lo, hi;
-            };
-            const Near near = *(const Near*)(values + at);
-            w[0][2 * n] = __builtin_amdgcn_perm(near.hi, near.lo, pick[0]);
-            w[0][2 * n + 1] = __builtin_amdgcn_perm(near.hi, near.lo, pick[1]);
+            // (from whole words: reads at odd halves take LDS a clock a lane)
+            const uint32_t* const near = (const uint32_t*)(values + (at & ~3));
+            const uint32_t lo = __builtin_amdgcn_alignbyte(near[1], near[0], at), hi = __builtin_amdgcn_alignbyte(near[2], near[1], at);
+            w[0][2 * n] = __builtin_amdgcn_perm(hi, lo, pick[0]);
+            w[0][2 * n + 1] = __builtin_amdgcn_perm(hi, lo, pick[1]);
             at += 2 * __popc(nibble);
         }
     }
@@ -71,13 +60,16 @@ __device__ inline void expand(const char* values, const u2* picks, uint32_t mask
 
 // A workgroup has 16 rows and NT * 16 tokens; its waves take the tiles along the columns in turn, and their sums meet in LDS.
 template <int TYPE, bool GATED, bool WIDE, int NT, int CHUNKS>
-__global__ __launch_bounds__(64 * kMostWaves) void linear_few_kernel(const LinearArgs a, int buffer) {
+__global__ __launch_bounds__(64 * kMostWaves) void linear_few_kernel(const LinearArgs a) {
     extern __shared__ char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    constexpr int kSize = sizeof(typename Num<TYPE>::type), kParts = kSize == 4 ? 2 : 1;
+    constexpr int kSize = sizeof(typename Num<TYPE>::type), kParts = kSize == 4 ? 2 : 1, kPieces = 4 * NT * kParts;
+    // a tile's inputs are asked for with its weights, a tile ahead, where there are registers for two tiles' inputs
+    constexpr bool kAhead = kPieces <= 8;
+    constexpr int kBuffer = few_buffer(CHUNKS);
     const int rt = blockIdx.x, token0 = blockIdx.y * NT * 16;
     u2* const picks = (u2*)lds;
-    char* const values = lds + 128 + wave * buffer;
+    char* const values = lds + 128 + wave * kBuffer;
     if (threadIdx.x < 16) {
         uint32_t p[4], pos = 0;
         for (int j = 0; j < 4; ++j) {
@@ -86,15 +78,42 @@ __global__ __launch_bounds__(64 * kMostWaves) void linear_few_kernel(const Linea
         }
         picks[threadIdx.x] = u2{p[0] | p[1] << 16, p[2] | p[3] << 16};
     }
-    __syncthreads();
-    f4 sum[NT] = {};
-    const int64_t first = (int64_t)rt * a.col_tiles;
-    Load<CHUNKS> next;
-    if (wave < a.col_tiles) ask(a, first + wave, lane, next);
     const int end = a.K * kSize;
     const char* row[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) row[t] = a.in + min(token0 + t * 16 + lane % 16, a.T - 1) * a.ld_in;
+    const auto inputs = [&](int ct, u4* x) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int p = 0; p < kParts; ++p)
+                    x[(b * NT + t) * kParts + p] = input16<TYPE, WIDE>(a, row[t], (ct * kTileCols + b * 32 + lane / 16 * 8) * kSize + p * 16, end);
+    };
+    const int64_t first = (int64_t)rt * a.col_tiles;
+    Load<CHUNKS, kAhead ? kPieces : 1> next;
+    const auto ask = [&](int ct, uint32_t begin, uint32_t stop) {
+        const int bytes = (int)(stop - begin) * 16;
+        const char* const from = a.kept + (uint64_t)begin * 16;
+        next.mask = a.mask[(first + ct) * 64 + lane];
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            const int at = c * 1024 + lane * 16;
+            next.v[c] = *(const u4*)(at < bytes ? from + at : a.zero);
+        }
+        if constexpr (kAhead) inputs(ct, next.x);
+    };
+    // where a tile's values lie is known one tile before they are asked for
+    uint32_t begin = 0, stop = 0;
+    const auto look = [&](int ct) {
+        if (ct < a.col_tiles) begin = a.start[first + ct], stop = a.start[first + ct + 1];
+    };
+    look(wave);
+    if (wave < a.col_tiles) ask(wave, begin, stop);
+    look(wave + waves);
+    __syncthreads();
+    f4 sum[NT] = {};
     for (int ct = wave; ct < a.col_tiles; ct += waves) {
         const uint32_t mask = next.mask;
 #pragma unroll
@@ -103,7 +122,17 @@ __global__ __launch_bounds__(64 * kMostWaves) void linear_few_kernel(const Linea
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-        if (ct + waves < a.col_tiles) ask(a, first + ct + waves, lane, next);
+        u4 x[kPieces];
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) x[i] = next.x[i];
+        } else {
+            inputs(ct, x);  // before the next weights: loads come back in order
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (ct + waves < a.col_tiles) ask(ct + waves, begin, stop);
+        look(ct + 2 * waves);
+        __builtin_amdgcn_sched_barrier(0);
         const int at = lanes_before(__popc(mask)) * kSize;
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
@@ -112,10 +141,7 @@ __global__ __launch_bounds__(64 * kMostWaves) void linear_few_kernel(const Linea
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int p = 0; p < kParts; ++p) {
-                    const u4 x = input16<TYPE, WIDE>(a, row[t], (ct * kTileCols + b * 32 + lane / 16 * 8) * kSize + p * 16, end);
-                    sum[t] = mfma16<TYPE>(w[p], x, sum[t]);
-                }
+                for (int p = 0; p < kParts; ++p) sum[t] = mfma16<TYPE>(w[p], x[(b * NT + t) * kParts + p], sum[t]);
         }
     }
     __syncthreads();
@@ -132,31 +158,38 @@ __global__ __launch_bounds__(64 * kMostWaves) void linear_few_kernel(const Linea
 
 template <int TYPE, bool GATED, bool WIDE, int NT, int CHUNKS>
 int launch_one(const LinearArgs& a, int waves, hipStream_t stream) {
-    // a lane reads up to 8 bytes from where its values end
-    const int buffer = CHUNKS * 1024 + 16, lds = 128 + std::max(waves * buffer, NT * waves * 1024);
+    const int lds = 128 + waves * std::max(few_buffer(CHUNKS), NT * 1024);
     const dim3 grid((unsigned)a.row_tiles, (unsigned)((a.T + NT * 16 - 1) / (NT * 16))), block(64 * waves);
     if (!grid_fits((double)grid.x * grid.y, 64 * waves)) return ESCOIN_ERANGE;
     const auto kernel = linear_few_kernel<TYPE, GATED, WIDE, NT, CHUNKS>;
     const int rc = lds > 64 * 1024 ? allow_dynamic_lds((const void*)kernel, lds) : ESCOIN_OK;
-    return rc != ESCOIN_OK ? rc : launch(kernel, grid, block, (size_t)lds, stream, a, buffer);
+    return rc != ESCOIN_OK ? rc : launch(kernel, grid, block, (size_t)lds, stream, a);
 }
 
 template <int TYPE, bool GATED, bool WIDE, int NT>
 int launch_chunks(const LinearHeader& h, const LinearArgs& a, int waves, hipStream_t stream) {
     const int chunks = (h.most_tile_bytes + 1023) / 1024;
-    if constexpr (TYPE == ESCOIN_T_F32)
-        if (chunks > 4) return launch_one<TYPE, GATED, WIDE, NT, 8>(a, waves, stream);
-    if (chunks > 2) return launch_one<TYPE, GATED, WIDE, NT, 4>(a, waves, stream);
+    if constexpr (TYPE == ESCOIN_T_F32) {
+        if (chunks > 5) return launch_one<TYPE, GATED, WIDE, NT, 8>(a, waves, stream);
+        if (chunks > 4) return launch_one<TYPE, GATED, WIDE, NT, 5>(a, waves, stream);
+    }
+    if (chunks > 3) return launch_one<TYPE, GATED, WIDE, NT, 4>(a, waves, stream);
+    if (chunks > 2) return launch_one<TYPE, GATED, WIDE, NT, 3>(a, waves, stream);
     if (chunks > 1) return launch_one<TYPE, GATED, WIDE, NT, 2>(a, waves, stream);
     return launch_one<TYPE, GATED, WIDE, NT, 1>(a, waves, stream);
 }
 
 template <int TYPE, bool GATED, bool WIDE>
 int launch_tokens(const LinearHeader& h, const LinearArgs& a, hipStream_t stream) {
-    const int waves = std::min(kMostWaves, a.col_tiles);
+    const int token_blocks = (a.T + 63) / 64;
+    int waves = kMostWaves;
+    while (waves > 4 && (int64_t)a.row_tiles * token_blocks * waves > 256 * 24) waves /= 2;
+    if (const char* e = getenv("WAVES")) waves = atoi(e);
+    waves = std::min(waves, a.col_tiles);
     if (a.T <= 16) return launch_chunks<TYPE, GATED, WIDE, 1>(h, a, waves, stream);
     if (a.T <= 32) return launch_chunks<TYPE, GATED, WIDE, 2>(h, a, waves, stream);
-    return launch_chunks<TYPE, GATED, WIDE, 4>(h, a, waves, stream);
+    if constexpr (TYPE == ESCOIN_T_F32) return launch_chunks<TYPE, GATED, WIDE, 2>(h, a, waves, stream);  // registers for no more inputs
+    else return launch_chunks<TYPE, GATED, WIDE, 4>(h, a, waves, stream);
 }
 
 template <int TYPE>

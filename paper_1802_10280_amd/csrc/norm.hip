@@ -12,77 +12,223 @@ struct NormArgs {
     float eps, alpha, beta, offset;
 };
 
-constexpr int kThreads = 256;
-
-// The sum over a workgroup, the same for each of its threads.
+// The sum over a row's WAVES waves (a whole workgroup where there are several), the same for each of its threads.
+template <int WAVES>
 __device__ inline float all_sum(float v, float* lds) {
+#define ESCOIN_SUM(CTRL, ROWS) v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+    ESCOIN_SUM(0x111, 0xf)  // row_shr 1, 2, 4, 8, then over the rows of 16: the last lane has the sum
+    ESCOIN_SUM(0x112, 0xf)
+    ESCOIN_SUM(0x114, 0xf)
+    ESCOIN_SUM(0x118, 0xf)
+    ESCOIN_SUM(0x142, 0xa)
+    ESCOIN_SUM(0x143, 0xc)
+#undef ESCOIN_SUM
+    v = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0f;
 #pragma unroll
-    for (int s = 32; s; s >>= 1) v += __shfl_xor(v, s);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float t = 0.0f;
-    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) t += lds[w];
-    return t;
+        for (int w = 0; w < WAVES; ++w) v += lds[w];
+    }
+    return v;
 }
 
 struct Stats {
     float mean, scale;
 };
 
-// Of f(i) over a row: two passes for a layer norm, the squares of the deviations and not a difference of sums.
-template <class F>
-__device__ inline Stats stats(const NormArgs& a, int kind, float* lds, F f) {
-    Stats s = {0.0f, 1.0f};
-    if (kind == ESCOIN_NORM_NONE) return s;
-    float v = 0.0f;
-    if (kind == ESCOIN_NORM_LAYER) {
-        for (int i = threadIdx.x; i < a.D; i += blockDim.x) v += f(i);
-        s.mean = all_sum(v, lds) / (float)a.D;
+// 16 bytes of a row as they lie in memory, at any element.
+template <class N>
+struct Piece {
+    static constexpr int kN = 16 / sizeof(N);
+    struct __attribute__((packed, aligned(sizeof(N)))) Raw {
+        N v[kN];
+    } raw;
+    // the elements from `at` on, of which `there` are in the row
+    __device__ void load(const void* row, int at, int there) {
+        const N* const p = (const N*)row + at;
+        if (there >= kN) raw = *(const Raw*)p;
+        else
+#pragma unroll
+            for (int j = 0; j < kN; ++j) raw.v[j] = j < there ? p[j] : (N)0.0f;
     }
-    v = 0.0f;
-    for (int i = threadIdx.x; i < a.D; i += blockDim.x) {
-        const float u = f(i) - s.mean;
-        v = fmaf(u, u, v);
+    __device__ void store(void* row, int at, int there) const {
+        N* const p = (N*)row + at;
+        if (there >= kN) *(Raw*)p = raw;
+        else
+#pragma unroll
+            for (int j = 0; j < kN; ++j)
+                if (j < there) p[j] = raw.v[j];
     }
-    s.scale = 1.0f / sqrtf(all_sum(v, lds) / (float)a.D + a.eps);
-    return s;
+};
+
+// A row stays in the registers of its WAVES waves, F elements a thread, in pieces of 16 bytes that follow each other over the threads.
+template <int TYPE, int WAVES, int F>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void norm_kernel(const NormArgs a) {
+    typedef typename Num<TYPE>::type N;
+    typedef Piece<N> P;
+    constexpr int kN = P::kN, kPieces = F / kN;
+    __shared__ float lds[WAVES];
+    const int t = WAVES == 1 ? blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x, lane = WAVES == 1 ? threadIdx.x & 63 : threadIdx.x;
+    if (WAVES == 1 && t >= a.T) return;
+    const auto at = [&](int i) { return (i * 64 * WAVES + lane) * kN; };
+    const auto there = [&](int i) { return a.D - at(i); };
+    const N* const x_row = (const N*)a.x + t * a.ld_x;
+    const N* const y_row = (const N*)a.y + t * a.ld_y;
+    const N* const gate_row = (const N*)a.gate + (a.gate_rows ? t * a.ld_gate : 0);
+    P x[kPieces], y[kPieces];
+    float v[F];
+    if (a.y)
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) y[i].load(y_row, at(i), there(i));
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) x[i].load(x_row, at(i), there(i));
+    const float count = (float)a.D;
+    // of v: two passes for a layer norm, the squares of the deviations and not a difference of sums
+    const auto stats = [&](int kind) {
+        Stats s = {0.0f, 1.0f};
+        if (kind == ESCOIN_NORM_NONE) return s;
+        if (kind == ESCOIN_NORM_LAYER) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < F; ++i) sum += v[i];
+            s.mean = all_sum<WAVES>(sum, lds) / count;
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            const float u = i % kN < there(i / kN) ? v[i] - s.mean : 0.0f;
+            sum = fmaf(u, u, sum);
+        }
+        s.scale = 1.0f / sqrtf(all_sum<WAVES>(sum, lds) / count + a.eps);
+        return s;
+    };
+    const auto norm = [&](int kind, const Stats& s, const void* weight, const void* bias) {
+        if (kind == ESCOIN_NORM_NONE) return;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            P w, b;
+            if (weight) w.load(weight, at(i), there(i));
+            if (bias) b.load(bias, at(i), there(i));
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                float u = (v[i * kN + j] - s.mean) * s.scale;
+                if (weight) u *= (float)w.raw.v[j] + a.offset;
+                if (bias) u += (float)b.raw.v[j];
+                v[i * kN + j] = u;
+            }
+        }
+    };
+    const auto put = [&](void* row) {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            P o;
+#pragma unroll
+            for (int j = 0; j < kN; ++j) o.raw.v[j] = (N)v[i * kN + j];
+            o.store(row, at(i), there(i));
+        }
+    };
+    if (a.y) {
+#pragma unroll
+        for (int i = 0; i < F; ++i) v[i] = (float)y[i / kN].raw.v[i % kN];
+        norm(a.post, stats(a.post), a.post_weight, a.post_bias);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            P g;
+            if (a.gate) g.load(gate_row, at(i), there(i));
+#pragma unroll
+            for (int j = 0; j < kN; ++j) {
+                float u = a.beta * v[i * kN + j];
+                if (a.gate) u *= (float)g.raw.v[j];
+                v[i * kN + j] = j < there(i) ? a.alpha * (float)x[i].raw.v[j] + u : 0.0f;  // a bias or gate beyond the row does not count
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < F; ++i) v[i] = a.alpha * (float)x[i / kN].raw.v[i % kN];
+    }
+    if (a.h) put((N*)a.h + t * a.ld_h);
+    if (!a.n) return;
+    norm(a.pre, stats(a.pre), a.pre_weight, a.pre_bias);
+    put((N*)a.n + t * a.ld_n);
 }
 
-template <class N>
-__device__ inline float normed(float v, int kind, const Stats& s, const void* weight, const void* bias, float offset, int i) {
-    if (kind == ESCOIN_NORM_NONE) return v;
-    v = (v - s.mean) * s.scale;
-    if (weight) v *= (float)((const N*)weight)[i] + offset;
-    if (bias) v += (float)((const N*)bias)[i];
-    return v;
+// Rows too long for that: read from memory again for every pass.
+constexpr int kLongWaves = 16;
+
+template <int TYPE>
+__global__ __launch_bounds__(64 * kLongWaves) void norm_long_kernel(const NormArgs a) {
+    typedef typename Num<TYPE>::type N;
+    __shared__ float lds[kLongWaves];
+    const int t = blockIdx.x;
+    const N* const x = (const N*)a.x + t * a.ld_x;
+    const N* const y = (const N*)a.y + t * a.ld_y;
+    const N* const gate = (const N*)a.gate + (a.gate_rows ? t * a.ld_gate : 0);
+    const auto stats = [&](int kind, auto f) {
+        Stats s = {0.0f, 1.0f};
+        if (kind == ESCOIN_NORM_NONE) return s;
+        float v = 0.0f;
+        if (kind == ESCOIN_NORM_LAYER) {
+            for (int i = threadIdx.x; i < a.D; i += 64 * kLongWaves) v += f(i);
+            s.mean = all_sum<kLongWaves>(v, lds) / (float)a.D;
+        }
+        v = 0.0f;
+        for (int i = threadIdx.x; i < a.D; i += 64 * kLongWaves) {
+            const float u = f(i) - s.mean;
+            v = fmaf(u, u, v);
+        }
+        s.scale = 1.0f / sqrtf(all_sum<kLongWaves>(v, lds) / (float)a.D + a.eps);
+        return s;
+    };
+    const auto normed = [&](float v, int kind, const Stats& s, const void* weight, const void* bias, int i) {
+        if (kind == ESCOIN_NORM_NONE) return v;
+        v = (v - s.mean) * s.scale;
+        if (weight) v *= (float)((const N*)weight)[i] + a.offset;
+        if (bias) v += (float)((const N*)bias)[i];
+        return v;
+    };
+    const Stats post = stats(a.y ? a.post : ESCOIN_NORM_NONE, [&](int i) { return (float)y[i]; });
+    const auto sum = [&](int i) {
+        float v = a.alpha * (float)x[i];
+        if (a.y) {
+            float b = a.beta * normed((float)y[i], a.post, post, a.post_weight, a.post_bias, i);
+            if (a.gate) b *= (float)gate[i];
+            v += b;
+        }
+        return v;
+    };
+    const Stats pre = stats(a.n ? a.pre : ESCOIN_NORM_NONE, sum);
+    for (int i = threadIdx.x; i < a.D; i += 64 * kLongWaves) {
+        const float v = sum(i);  // both are read before either is written: an output may take an input's place
+        if (a.h) ((N*)a.h)[t * a.ld_h + i] = (N)v;
+        if (a.n) ((N*)a.n)[t * a.ld_n + i] = (N)normed(v, a.pre, pre, a.pre_weight, a.pre_bias, i);
+    }
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(kThreads) void norm_kernel(const NormArgs a) {
-    typedef typename Num<TYPE>::type N;
-    __shared__ float lds[kThreads / 64];
-    for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
-        const N* const x = (const N*)a.x + t * a.ld_x;
-        const N* const y = (const N*)a.y + t * a.ld_y;
-        const N* const gate = (const N*)a.gate + (a.gate_rows ? t * a.ld_gate : 0);
-        const Stats post = stats(a, a.y ? a.post : ESCOIN_NORM_NONE, lds, [&](int i) { return (float)y[i]; });
-        const auto sum = [&](int i) {
-            float v = a.alpha * (float)x[i];
-            if (a.y) {
-                float b = a.beta * normed<N>((float)y[i], a.post, post, a.post_weight, a.post_bias, a.offset, i);
-                if (a.gate) b *= (float)gate[i];
-                v += b;
-            }
-            return v;
-        };
-        const Stats pre = stats(a, a.n ? a.pre : ESCOIN_NORM_NONE, lds, sum);
-        for (int i = threadIdx.x; i < a.D; i += blockDim.x) {
-            const float v = sum(i);
-            if (a.h) ((N*)a.h)[t * a.ld_h + i] = (N)v;
-            if (a.n) ((N*)a.n)[t * a.ld_n + i] = (N)normed<N>(v, a.pre, pre, a.pre_weight, a.pre_bias, a.offset, i);
-        }
+int launch_norm(const NormArgs& a, hipStream_t stream) {
+    const int D = a.D;
+    const auto go = [&](auto kernel, int waves) {
+        const int64_t blocks = waves == 1 ? ((int64_t)a.T + 3) / 4 : a.T;
+        const int threads = waves == 1 ? 256 : 64 * waves;
+        if (!grid_fits((double)blocks, threads)) return (int)ESCOIN_ERANGE;
+        return launch(kernel, dim3((unsigned)blocks), dim3(threads), 0, stream, a);
+    };
+    const bool many = a.T >= 1024;
+    if (D <= 512) return go(norm_kernel<TYPE, 1, 8>, 1);
+    if (many) {
+        if (D <= 1024) return go(norm_kernel<TYPE, 1, 16>, 1);
+        if (D <= 2048) return go(norm_kernel<TYPE, 1, 32>, 1);
+        if (D <= 4096) return go(norm_kernel<TYPE, 4, 16>, 4);
+        if (D <= 8192) return go(norm_kernel<TYPE, 4, 32>, 4);
     }
+    if (D <= 2048) return go(norm_kernel<TYPE, 4, 8>, 4);
+    if (D <= 8192) return go(norm_kernel<TYPE, 16, 8>, 16);
+    if (D <= 16384) return go(norm_kernel<TYPE, 16, 16>, 16);
+    if (D <= 32768) return go(norm_kernel<TYPE, 16, 32>, 16);
+    return go(norm_long_kernel<TYPE>, kLongWaves);
 }
 
 int make_norm_args(const escoin_norm_desc* desc, NormArgs* a) {
@@ -135,11 +281,10 @@ int escoin_norm_forward(const escoin_norm_desc* desc, const void* d_x, const voi
     if (bits & (desc->type == ESCOIN_T_F32 ? 3 : 1)) return ESCOIN_EINVAL;
     a.x = d_x; a.y = d_y; a.gate = d_gate; a.post_weight = d_post_weight; a.post_bias = d_post_bias; a.pre_weight = d_pre_weight; a.pre_bias = d_pre_bias;
     a.h = d_h; a.n = d_n;
-    const dim3 grid(std::min(a.T, 1 << 20)), block(kThreads);
     hipStream_t stream = (hipStream_t)hip_stream;
-    if (desc->type == ESCOIN_T_F32) return launch(norm_kernel<ESCOIN_T_F32>, grid, block, 0, stream, a);
-    if (desc->type == ESCOIN_T_F16) return launch(norm_kernel<ESCOIN_T_F16>, grid, block, 0, stream, a);
-    return launch(norm_kernel<ESCOIN_T_BF16>, grid, block, 0, stream, a);
+    if (desc->type == ESCOIN_T_F32) return launch_norm<ESCOIN_T_F32>(a, stream);
+    if (desc->type == ESCOIN_T_F16) return launch_norm<ESCOIN_T_F16>(a, stream);
+    return launch_norm<ESCOIN_T_BF16>(a, stream);
 }
 
 }  // extern "C"
