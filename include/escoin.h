@@ -231,7 +231,7 @@ typedef struct escoin_linear_desc {
 } escoin_linear_desc;
 
 /* Validates a descriptor: ESCOIN_EINVAL for T < 0, K or M < 1, an unknown type or a row pitch shorter than its row,
- * ESCOIN_ERANGE where 2*M or K reaches 2^30 or a pitch 2^40. */
+ * ESCOIN_ERANGE where K reaches 2^22, 2*M 2^30 or a pitch 2^40, or the 16 by 128 tiles of the weights 2^31. */
 int escoin_linear_check_desc(const escoin_linear_desc *desc);
 
 /*
@@ -254,7 +254,7 @@ int escoin_linear_plan_build(const escoin_linear_desc *desc, const int32_t *rowp
 /*
  * One forward call.  Up to escoin_linear_few_tokens tokens a kernel reads each kept weight once and multiplies it on the
  * matrix cores as it comes, beyond that the weights are multiplied in tiles, zeros too.  Pruned weights count as zeros: an Inf
- * or NaN in a token's input makes every output of that token NaN (or what the epilogue makes of it), and of no other token.
+ * or NaN in a token's input can make every output of that token NaN (or what the epilogue makes of it), and of no other token.
  * The order of the sums depends on T, never on timing: equal calls give equal bits.
  *   plan_host     host pointer to the blob (its header is read at the call), d_plan its copy on the device, 16-byte aligned
  *   d_bias        device, M (gated: 2*M) elements, with ESCOIN_F_BIAS

@@ -247,34 +247,39 @@ def make_norm_desc(T, D, type, post=NORM_NONE, pre=NORM_RMS, gate_rows=0, eps=1e
     return escoin_norm_desc(T, D, type, post, pre, gate_rows, eps, alpha, beta, weight_offset, ld_x, ld_y, ld_gate, ld_h, ld_n)
 
 
-def _torch_type(type):
-    import torch
-    return (torch.float32, torch.float16, torch.bfloat16)[type]
+_torch_types = []
 
 
 class _Rows:
-    """Checks the device tensors of one call: all on one device, of one type; rows of contiguous elements, or vectors."""
+    """Checks the device tensors of one call: all on one device, of one type; rows of contiguous elements, or vectors.  A call
+    of one token takes some microseconds: the checks are few and cheap."""
+    __slots__ = ("type", "device")
 
     def __init__(self, type):
-        self.type, self.device = _torch_type(type), None
+        if not _torch_types:
+            import torch
+            _torch_types.extend((torch.float32, torch.float16, torch.bfloat16))
+        self.type, self.device = _torch_types[type], -1
 
     def _seen(self, t):
-        if not t.is_cuda:
-            raise TypeError("device arguments must be CUDA tensors")
-        if t.dtype != self.type:
+        if t.dtype is not self.type:
             raise TypeError(f"device tensor has dtype {t.dtype}, expected {self.type}")
-        if self.device is None:
-            self.device = t.device
-        elif t.device != self.device:
-            raise TypeError(f"tensors of one call lie on {self.device} and on {t.device}")
+        device = t.get_device()
+        if device < 0:
+            raise TypeError("device arguments must be CUDA tensors")
+        if device != self.device:
+            if self.device >= 0:
+                raise TypeError(f"tensors of one call lie on devices {self.device} and {device}")
+            self.device = device
 
     def rows(self, t, T, width, ld):
         """Pointer to T rows of `width` elements, `ld` (0: width) apart, or None."""
         if t is None:
             return None
         self._seen(t)
-        if t.dim() != 2 or t.shape[0] < T or t.shape[1] != width or (width > 1 and t.stride(1) != 1) or (T > 1 and t.stride(0) != (ld or width)):
-            raise TypeError(f"expected {T} rows of {width}, {ld or width} elements apart: got shape {tuple(t.shape)}, strides {t.stride()}")
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 2 or shape[0] < T or shape[1] != width or (width > 1 and stride[1] != 1) or (T > 1 and stride[0] != (ld or width)):
+            raise TypeError(f"expected {T} rows of {width}, {ld or width} elements apart: got shape {tuple(shape)}, strides {stride}")
         return t.data_ptr()
 
     def vector(self, t, width):
@@ -288,10 +293,12 @@ class _Rows:
     def call(self, where, fn, *args, stream):
         """The library launches on the current device: the tensors' own for the time of the call."""
         import torch
-        if self.device.index != torch.cuda.current_device():
+        if self.device != torch.cuda.current_device():
             with torch.cuda.device(self.device):
                 return _check(fn(*args, _stream(stream)), where)
-        _check(fn(*args, _stream(stream)), where)
+        rc = fn(*args, torch._C._cuda_getCurrentRawStream(self.device) if stream is None else _stream(stream))
+        if rc != OK:
+            _check(rc, where)
 
 
 def escoin_linear_check_desc(desc) -> int:
@@ -340,10 +347,13 @@ class _LinearHeader(ctypes.Structure):
                 + [(k, ctypes.c_uint64) for k in ("off_zero", "off_mask", "off_start", "off_kept", "off_whole", "total_bytes")])
 
 
+_BYTES, _HEADER_BYTES = np.dtype(np.uint8), ctypes.sizeof(_LinearHeader)
+
+
 def _plan_ptr(plan: np.ndarray):
-    if plan is not None and plan.nbytes < ctypes.sizeof(_LinearHeader):
+    if not isinstance(plan, np.ndarray) or plan.dtype != _BYTES or not plan.flags.c_contiguous or plan.nbytes < _HEADER_BYTES:
         raise TypeError("this is no plan of a linear layer")
-    return _hptr(plan, np.uint8)
+    return plan.__array_interface__["data"][0]
 
 
 def linear_plan_header(plan: np.ndarray) -> dict:
@@ -357,10 +367,10 @@ def escoin_linear_forward(desc, plan_host: np.ndarray, d_plan, d_in, d_out, d_bi
     T, rows = max(desc.T, 0), desc.M * (2 if desc.gated else 1)
     args = (t.rows(d_in, T, desc.K, desc.ld_in), t.rows(d_out, T, desc.M, desc.ld_out), t.vector(d_bias, rows),
             t.rows(d_residual, T, desc.M, desc.ld_residual))
-    if d_plan.device != t.device or d_plan.nbytes < plan_host.nbytes:
+    plan = _plan_ptr(plan_host)
+    if d_plan.get_device() != t.device or d_plan.nbytes < plan_host.nbytes or not d_plan.is_contiguous():
         raise TypeError("the plan's copy has to be whole and on the tensors' device")
-    t.call("escoin_linear_forward", lib().escoin_linear_forward, ctypes.byref(desc), _plan_ptr(plan_host), d_plan.data_ptr(), *args, flags,
-           stream=stream)
+    t.call("escoin_linear_forward", lib().escoin_linear_forward, ctypes.byref(desc), plan, d_plan.data_ptr(), *args, flags, stream=stream)
 
 
 def escoin_norm_check_desc(desc) -> int:

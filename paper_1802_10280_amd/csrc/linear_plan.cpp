@@ -153,11 +153,11 @@ int make_linear_dims(const escoin_linear_desc* desc, LinearDims* d) {
     const escoin_linear_desc& p = *desc;
     if (p.T < 0 || p.K < 1 || p.M < 1 || p.type < ESCOIN_T_F32 || p.type > ESCOIN_T_BF16 || (p.gated & ~1)) return ESCOIN_EINVAL;
     if (!pitch(p.ld_in, p.K, &d->ld_in) || !pitch(p.ld_out, p.M, &d->ld_out) || !pitch(p.ld_residual, p.M, &d->ld_residual)) return ESCOIN_EINVAL;
-    if (p.K >= 1 << 30 || p.M >= 1 << 29) return ESCOIN_ERANGE;
+    if (p.K >= 1 << 22 || p.M >= 1 << 29) return ESCOIN_ERANGE;
     if (d->ld_in >= 1ll << 40 || d->ld_out >= 1ll << 40 || d->ld_residual >= 1ll << 40) return ESCOIN_ERANGE;
     d->T = p.T; d->K = p.K; d->M = p.M; d->type = p.type; d->gated = p.gated != 0;
-    // the kernels count tiles, and the fragments of a row block, in 32 bits; starts are kept in units of 16 bytes
-    if ((double)d->row_tiles() * d->col_tiles() >= 0x1p31 || (double)d->col_frags() * kFragBytes >= 0x1p31) return ESCOIN_ERANGE;
+    // tiles are counted in 32 bits, and so are the bytes of 256 rows of whole weights: K stays below 2^22
+    if ((double)d->row_tiles() * d->col_tiles() >= 0x1p31) return ESCOIN_ERANGE;
     return ESCOIN_OK;
 }
 

@@ -112,7 +112,7 @@ def test_linear_descriptors():
     assert esc.escoin_linear_check_desc(esc.make_linear_desc(**{**ok, "T": 0})) == esc.OK
     for bad in (dict(T=-1), dict(K=0), dict(M=-5), dict(type=3), dict(type=-1), dict(gated=2), dict(ld_in=9), dict(ld_out=3), dict(ld_residual=-4)):
         assert esc.escoin_linear_check_desc(esc.make_linear_desc(**{**ok, **bad})) == esc.EINVAL, bad
-    for far in (dict(K=1 << 30), dict(M=1 << 29), dict(ld_in=1 << 40), dict(K=(1 << 30) - 1, M=1 << 28)):
+    for far in (dict(K=1 << 22), dict(M=1 << 29), dict(ld_in=1 << 40), dict(K=(1 << 22) - 1, M=1 << 28)):
         assert esc.escoin_linear_check_desc(esc.make_linear_desc(**{**ok, **far})) == esc.ERANGE, far
     assert esc.lib().escoin_linear_check_desc(None) == esc.EINVAL
 
@@ -192,3 +192,91 @@ def test_the_convolutions_refuse_the_new_flags():
     one = ctypes.c_void_p(256)
     for flag in (esc.F_RESIDUAL, esc.F_SILU, esc.F_GELU, esc.F_GELU_TANH):
         assert esc.lib().escoin_sconv_forward(ctypes.byref(d), one, one, one, one, one, one, flag, None) == esc.EINVAL
+
+
+class Tensor:
+    """What the binding looks at of a device tensor, without a device."""
+
+    def __init__(self, shape, type=2, device=0, stride=None):
+        self.shape, self.dtype, self.device = tuple(shape), ff.torch_type(type), device
+        self.strides = stride or tuple(int(np.prod(shape[i + 1:])) for i in range(len(shape)))
+
+    def get_device(self):
+        return self.device
+
+    def stride(self):
+        return self.strides
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def is_contiguous(self):
+        return self.strides == tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+    @property
+    def nbytes(self):
+        return self.numel() * (4 if self.dtype == ff.torch_type(0) else 2)
+
+    def data_ptr(self):
+        return 4096
+
+
+class Reached(Exception):
+    pass
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
+    """Every refusal is raised before the library is called; the calls that are not refused reach it."""
+    from paper_1802_10280_amd import binding
+
+    def call(self, where, fn, *args, stream):
+        raise Reached
+
+    monkeypatch.setattr(binding._Rows, "call", call)
+    T, K, M = 4, 64, 16
+    d = esc.make_linear_desc(T, K, M, esc.T_BF16)
+    _, csr = ff.pruned(M, K, 0.5, 1, 2)
+    plan = esc.escoin_linear_plan_build(d, *csr)
+    ok = dict(plan_host=plan, d_plan=Tensor([plan.nbytes // 2]), d_in=Tensor([T, K]), d_out=Tensor([T, M]), d_bias=Tensor([M]), d_residual=Tensor([T, M]))
+    for good in ({}, dict(d_bias=None, d_residual=None), dict(d_in=Tensor([T + 1, K])), dict(d_plan=Tensor([plan.nbytes]))):
+        with pytest.raises(Reached):
+            esc.escoin_linear_forward(d, **{**ok, **good})
+    for name, t in ok.items():
+        if name == "plan_host":
+            bad = [None, plan[:40], plan.astype(np.int8), plan[::2]]
+        elif name == "d_plan":
+            bad = [Tensor([plan.nbytes // 2], device=-1), Tensor([plan.nbytes // 2], device=1), Tensor([plan.nbytes // 2 - 1]), Tensor([plan.nbytes // 2], stride=(2,))]
+        else:
+            s = t.shape
+            bad = [Tensor(s, 0), Tensor(s, 1), Tensor(s, device=-1), Tensor(s[:-1] + (s[-1] - 1,)), Tensor(s[:-1] + (s[-1] + 1,))]
+            if len(s) == 2:
+                bad += [Tensor((T - 1, s[1])), Tensor(s, stride=(1, T)), Tensor(s, stride=(s[1] + 1, 1)), Tensor((T * s[1],))]
+            else:
+                bad += [Tensor(s, stride=(2,))]
+            if name != "d_in":
+                bad += [Tensor(s, device=1)]
+        for b in bad:
+            with pytest.raises(TypeError):
+                esc.escoin_linear_forward(d, **{**ok, name: b})
+    wide = esc.make_linear_desc(T, K, M, esc.T_BF16, ld_in=K + 8)
+    with pytest.raises(Reached):
+        esc.escoin_linear_forward(wide, **{**ok, "d_in": Tensor([T, K], stride=(K + 8, 1))})
+    with pytest.raises(TypeError):
+        esc.escoin_linear_forward(wide, **ok)
+
+    D = 24
+    for rows in (0, 1):
+        d = esc.make_norm_desc(T, D, esc.T_BF16, esc.NORM_RMS, esc.NORM_RMS, rows)
+        gate = [T, D] if rows else [D]
+        ok = dict(d_x=Tensor([T, D]), d_h=Tensor([T, D]), d_n=Tensor([T, D]), d_y=Tensor([T, D]), d_gate=Tensor(gate), d_post_weight=Tensor([D]),
+                  d_post_bias=Tensor([D]), d_pre_weight=Tensor([D]), d_pre_bias=Tensor([D]))
+        for good in ({}, dict(d_h=None), dict(d_n=None, d_pre_bias=None), dict(d_gate=None)):
+            with pytest.raises(Reached):
+                esc.escoin_norm_forward(d, **{**ok, **good})
+        for name, t in ok.items():
+            s = t.shape
+            bad = [Tensor(s, 1), Tensor(s, device=-1), Tensor(s, device=1) if name != "d_gate" else Tensor(s, 0), Tensor(s[:-1] + (D - 1,)), Tensor(s[:-1] + (D + 1,))]
+            bad += [Tensor((T - 1, D)), Tensor(s, stride=(1, T)), Tensor((T * D,))] if len(s) == 2 else [Tensor(s, stride=(2,)), Tensor((T, D))]
+            for b in bad:
+                with pytest.raises(TypeError):
+                    esc.escoin_norm_forward(d, **{**ok, name: b})
