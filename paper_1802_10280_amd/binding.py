@@ -343,7 +343,7 @@ def escoin_linear_few_tokens(desc, plan_host: np.ndarray) -> int:
 class _LinearHeader(ctypes.Structure):
     """Mirror of the linear plan's header (csrc/linear.h), for diagnostics and tests."""
     _fields_ = ([(k, ctypes.c_uint32) for k in ("magic", "version")]
-                + [(k, ctypes.c_int32) for k in ("K", "M", "type", "gated", "most_tokens", "few_tokens", "most_tile_bytes", "reserved")]
+                + [(k, ctypes.c_int32) for k in ("K", "M", "type", "gated", "most_tokens", "few_tokens", "most_lane_words", "reserved")]
                 + [(k, ctypes.c_uint64) for k in ("off_zero", "off_mask", "off_start", "off_kept", "off_whole", "total_bytes")])
 
 

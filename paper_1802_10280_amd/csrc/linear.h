@@ -25,7 +25,7 @@ struct LinearHeader {
     int32_t K, M, type, gated;
     int32_t most_tokens;    // of a call
     int32_t few_tokens;     // up to so many the kept weights are read; most_tokens above it: the whole ones are there too
-    int32_t most_tile_bytes;// values of the fullest tile
+    int32_t most_lane_words;// 32-bit words that the fullest lane's values of a tile touch
     int32_t reserved;
     uint64_t off_zero;      // 256 bytes of zeros
     uint64_t off_mask;      // [row tile][column tile][lane], 32 bits

@@ -12,6 +12,18 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 
+typedef __attribute__((address_space(3))) void* Lds;
+typedef __amdgpu_buffer_rsrc_t Buffer;
+
+// Memory by way of a buffer: offsets of 32 bits, zeros where the lane's own one reaches `bytes`.
+__device__ inline Buffer buffer(const char* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000); }
+__device__ inline u4 load16(Buffer from, int lane_offset, int offset) { return __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset, offset, 0); }
+
+// 16 bytes a lane: 1024 of LDS from `to` on
+__device__ inline void copy16(Buffer from, int lane_offset, int offset, char* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Lds)to, 16, lane_offset, offset, 0, 0);
+}
+
 template <int TYPE>
 struct Num;
 template <>
@@ -54,45 +66,68 @@ __device__ inline f16v mfma32(u4 w, u4 x, f16v c) {
     }
 }
 
-__device__ inline float activate(float z, uint32_t flags) {
-    if (flags & ESCOIN_F_RELU) return z > 0.0f ? z : 0.0f;
-    if (flags & ESCOIN_F_SILU) return z / (1.0f + expf(-z));
-    if (flags & ESCOIN_F_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-    // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), which keeps its bits where tanh is near -1
-    if (flags & ESCOIN_F_GELU_TANH) return z / (1.0f + expf(-1.5957691216057308f * (z + 0.044715f * z * z * z)));
-    return z;
+// z / (1 + exp(-u)).  For outputs of 16 bits the instructions' own exponential and reciprocal, each a step of fp32 or two off, do; the
+// library's forms, some 40 instructions, are an eighth of a long prompt's time.
+template <int TYPE>
+__device__ inline float logistic(float z, float u) {
+    if constexpr (TYPE == ESCOIN_T_F32) return z / (1.0f + expf(-u));
+    else return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * u));
 }
 
 template <int TYPE>
-__device__ inline float number(const char* p, int64_t i) {
-    return (float)((const typename Num<TYPE>::type*)p)[i];
+__device__ inline float activate(float z, uint32_t flags) {
+    if (flags & ESCOIN_F_RELU) return z > 0.0f ? z : 0.0f;
+    if (flags & ESCOIN_F_SILU) return logistic<TYPE>(z, z);
+    if (flags & ESCOIN_F_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
+    // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), which keeps its bits where tanh is near -1
+    if (flags & ESCOIN_F_GELU_TANH) return logistic<TYPE>(z, 1.5957691216057308f * (z + 0.044715f * z * z * z));
+    return z;
 }
 
-// What follows the sums of four neighbouring rows (from `row`, a multiple of four) for one token: bias, activation, gate,
+// What follows the sums of R * 4 neighbouring rows (from `row`, a multiple of R * 4) for one token: bias, activation, gate,
 // residual, and the store.  A gated layer's rows are a gate, its partner, the next gate, its partner.
-template <int TYPE, bool GATED>
-__device__ inline void finish(const LinearArgs& a, f4 z, int row, int token) {
+template <int TYPE, bool GATED, int R>
+__device__ inline void finish(const LinearArgs& a, const f4 (&z)[R], int row, int token) {
     typedef typename Num<TYPE>::type N;
     if (token >= a.T || row >= a.rows) return;
-    constexpr int kOut = GATED ? 2 : 4;
+    constexpr int kOut = GATED ? 2 * R : 4 * R;
+    typedef N Nv __attribute__((ext_vector_type(kOut)));
     const int m0 = GATED ? row >> 1 : row;
-    N* const out = (N*)(a.out + token * a.ld_out) + m0;
-    const N* const residual = (const N*)(a.residual + token * a.ld_residual) + m0;
-    float v[kOut];
+    const bool whole = m0 + kOut <= a.M;
+    // as many neighbours as there are, by element where they end or where they do not start on their size
+    const auto get = [&](const char* p, N (&to)[kOut]) {
+        if (whole && ((uintptr_t)p & (kOut * sizeof(N) - 1)) == 0) {
+            const Nv v = *(const Nv*)p;
 #pragma unroll
-    for (int i = 0; i < kOut; ++i) {
-        if (m0 + i >= a.M) break;
-        if constexpr (GATED) {
-            float g = z[2 * i], u = z[2 * i + 1];
-            if (a.bias) g += number<TYPE>(a.bias, m0 + i), u += number<TYPE>(a.bias, a.M + m0 + i);
-            v[i] = activate(g, a.flags) * u;
+            for (int i = 0; i < kOut; ++i) to[i] = v[i];
         } else {
-            v[i] = activate(a.bias ? z[i] + number<TYPE>(a.bias, m0 + i) : z[i], a.flags);
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) to[i] = m0 + i < a.M ? ((const N*)p)[i] : (N)0.0f;
         }
-        if (a.residual) v[i] += (float)residual[i];
+    };
+    float v[kOut];
+    N b[kOut];
+    if constexpr (GATED) {
+        N c[kOut];
+        if (a.bias) get(a.bias + m0 * sizeof(N), b), get(a.bias + ((int64_t)a.M + m0) * sizeof(N), c);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) {
+            float g = z[i / 2][i % 2 * 2], u = z[i / 2][i % 2 * 2 + 1];
+            if (a.bias) g += (float)b[i], u += (float)c[i];
+            v[i] = activate<TYPE>(g, a.flags) * u;
+        }
+    } else {
+        if (a.bias) get(a.bias + m0 * sizeof(N), b);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) v[i] = activate<TYPE>(a.bias ? z[i / 4][i % 4] + (float)b[i] : z[i / 4][i % 4], a.flags);
     }
-    if (m0 + kOut <= a.M && ((uintptr_t)out & (kOut * sizeof(N) - 1)) == 0) {
-        typedef N Nv __attribute__((ext_vector_type(kOut)));
+    if (a.residual) {
+        get(a.residual + token * a.ld_residual + m0 * sizeof(N), b);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) v[i] += (float)b[i];
+    }
+    N* const out = (N*)(a.out + token * a.ld_out) + m0;
+    if (whole && ((uintptr_t)out & (kOut * sizeof(N) - 1)) == 0) {
         Nv o;
 #pragma unroll
         for (int i = 0; i < kOut; ++i) o[i] = (N)v[i];
@@ -104,6 +139,15 @@ __device__ inline void finish(const LinearArgs& a, f4 z, int row, int token) {
     }
 }
 
+// 16 bytes from any element on
+template <int TYPE>
+__device__ inline u4 any16(const char* p) {
+    struct __attribute__((packed, aligned(sizeof(typename Num<TYPE>::type)))) Raw {
+        u4 v;
+    };
+    return ((const Raw*)p)->v;
+}
+
 // 16 bytes of a token's row from byte `at` on, zeros beyond `end`.  WIDE: rows start on 16 bytes and hold a multiple of them.
 template <int TYPE, bool WIDE>
 __device__ inline u4 input16(const LinearArgs& a, const char* row, int at, int end) {
@@ -112,10 +156,7 @@ __device__ inline u4 input16(const LinearArgs& a, const char* row, int at, int e
     } else {
         typedef typename Num<TYPE>::type N;
         constexpr int kN = 16 / sizeof(N);
-        struct __attribute__((packed, aligned(sizeof(N)))) Raw {
-            u4 v;
-        };
-        if (at + 16 <= end) return ((const Raw*)(row + at))->v;
+        if (at + 16 <= end) return any16<TYPE>(row + at);
         typedef N Nv __attribute__((ext_vector_type(kN)));
         Nv v = {};
         if (at < end)
@@ -128,8 +169,9 @@ __device__ inline u4 input16(const LinearArgs& a, const char* row, int at, int e
 
 }  // namespace
 
+// Whether inputs come by wide loads: rows on 16 bytes that hold a multiple of them, and a tile's rows within 32 bits of offsets.
 inline bool wide_input(const LinearArgs& a, int size) {
-    return (((uintptr_t)a.in | (uintptr_t)a.ld_in | (uintptr_t)((int64_t)a.K * size)) & 15) == 0;
+    return (((uintptr_t)a.in | (uintptr_t)a.ld_in | (uintptr_t)((int64_t)a.K * size)) & 15) == 0 && a.ld_in < 1 << 23;
 }
 
 }  // namespace escoin

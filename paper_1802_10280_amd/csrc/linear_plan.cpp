@@ -38,8 +38,22 @@ inline uint16_t fp16_bits(float f) {
     return (uint16_t)(sign | (q + (rest > half || (rest == half && (q & 1)) ? 1 : 0)));
 }
 
-// Up to how many tokens the kept weights are read.
-int few_tokens(const LinearDims&) { return 64; }
+// Up to how many tokens the kept weights are read.  Every workgroup unfolds them for itself, for 64 tokens at a time (fp32: 32): microseconds
+// a tile and compute unit.  The tiled kernel's time is its steps (linear_many.hip), but no less than the whole weights take from memory;
+// it needs rows enough to be spread over the compute units.  Measured with 64 tokens at 50 %, kept against whole: 12288 to 4096 34
+// and 53 us, 2560 to 2560 10.7 and 11, 4096 to 24576 73 and 34, at 32 tokens 37.7 and 32.1 (41 from memory).
+int few_tokens(const LinearDims& d) {
+    const bool f32 = d.type == ESCOIN_T_F32;
+    const double tiles = (double)d.row_tiles() * d.col_tiles() / 256, steps = d.col_frags() / kStepFrags;
+    const double memory = (double)d.row_frags() * d.col_frags() * kFragBytes / 4.9e6;
+    int most = 16;
+    for (int T = 32; T <= 256; T += 32) {
+        const double kept = f32 ? 0.61 * (T / 32) : T <= 32 ? 0.18 : 0.30 * ((T + 63) / 64);
+        const double rounds = (double)((((d.rows() + 63) / 64) * (int64_t)(T / 32) + 255) / 256);
+        if (kept * tiles <= std::max(memory, (f32 ? 0.27 : 0.155) * steps * rounds)) most = T;
+    }
+    return most;
+}
 
 int check_csr(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx) {
     if (!rowptr || rowptr[0] != 0) return ESCOIN_EINVAL;
@@ -67,7 +81,7 @@ LinearHeader layout(const LinearDims& d, int32_t nnz) {
     h.off_mask = h.off_zero + 256;
     h.off_start = h.off_mask + tiles * 256;
     h.off_kept = up(h.off_start + (tiles + 1) * 4, 256);
-    h.off_whole = up(h.off_kept + (uint64_t)nnz * d.size() + tiles * 15, 256);
+    h.off_whole = up(h.off_kept + (uint64_t)nnz * d.size() + tiles * 15 + 16, 256);  // 16: a lane reads over its tile's end
     h.total_bytes = h.off_whole;
     if (d.T > h.few_tokens) h.total_bytes += (uint64_t)d.row_frags() * d.col_frags() * kFragBytes;
     return h;
@@ -113,7 +127,6 @@ int fill(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, cons
             for (int ct = 0; ct < d.col_tiles(); ++ct) {
                 const size_t tile = (size_t)rt * d.col_tiles() + ct;
                 start[tile] = (uint32_t)(at / 16);
-                const uint64_t begin = at;
                 for (int lane = 0; lane < 64; ++lane) {
                     const V* const from = dense.get() + (size_t)(half * kTileRows + lane % 16) * cols + ct * kTileCols + lane / 16 * 8;
                     uint32_t bits = 0;
@@ -126,10 +139,10 @@ int fill(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, cons
                             bits |= 1u << (b * 8 + j);
                             to[n++] = v;
                         }
+                    most = std::max(most, (int)((at % 4 + n * sizeof(V) + 3) / 4));
                     at += n * sizeof(V);
                     mask[tile * 64 + lane] = bits;
                 }
-                most = std::max(most, (int)(at - begin));
                 while (at % 16) kept[at++] = 0;
             }
         }
@@ -142,7 +155,7 @@ int fill(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, cons
     }
     start[(size_t)d.row_tiles() * d.col_tiles()] = (uint32_t)(at / 16);
     memset(kept + at, 0, (size_t)(h->off_whole - h->off_kept - at));
-    h->most_tile_bytes = most;
+    h->most_lane_words = most;
     return ESCOIN_OK;
 }
 

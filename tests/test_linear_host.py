@@ -32,16 +32,19 @@ def decode_kept(plan, h, rows, K):
     for r in range(rt):
         for c in range(ct):
             t = r * ct + c
-            n = sum(int(m).bit_count() if hasattr(int, "bit_count") else bin(int(m)).count("1") for m in mask[r, c])
+            n = sum(bin(int(m)).count("1") for m in mask[r, c])
             at = h["off_kept"] + int(start[t]) * 16
             assert int(start[t + 1]) * 16 - int(start[t]) * 16 == -(-n * size // 16) * 16
-            most = max(most, n * size)
             values = iter(unrounded(plan[at:at + n * size], h["type"]))
+            begin = 0
             for lane in range(64):
+                n = bin(int(mask[r, c, lane])).count("1")
+                most = max(most, (begin % 4 + n * size + 3) // 4)
+                begin += n * size
                 for bit in range(32):
                     if mask[r, c, lane] >> bit & 1:
                         out[r * 16 + lane % 16, c * 128 + bit // 8 * 32 + lane // 16 * 8 + bit % 8] = next(values)
-    assert most == h["most_tile_bytes"]
+    assert most == h["most_lane_words"]
     return out
 
 
