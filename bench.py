@@ -41,7 +41,8 @@ def parse():
     ap.add_argument("--warmup", type=int, default=20)
     ap.add_argument("--workload", default="resnet",
                     help="one of workloads.CONFIG_LAYERS or a comma list of layer names; `chain` "
-                         "feeds every layer's output (bias + ReLU fused) to the next layer")
+                         "feeds every layer's output (bias + ReLU fused) to the next layer; `feedforward` "
+                         "(workloads.CONFIG_BLOCKS) times feed-forward blocks of pruned linear layers")
     ap.add_argument("--path", default=os.environ.get("ESCOIN_BENCH_PATH", "auto"),
                     choices=["auto", "direct", "tiled"], help="which sconv entry point `value` times")
     ap.add_argument("--flags", type=int, default=0, help="1 = bias, 2 = relu (fused epilogue)")
@@ -161,6 +162,10 @@ def main():
     esc.lib()  # fail loudly if the HIP library is missing
     assert torch.cuda.is_available(), "bench.py needs a GPU"
     torch.cuda.set_device(0)
+
+    if args.workload in wl.CONFIG_BLOCKS:
+        print(json.dumps(feedforward(torch, wl, args)))
+        return
 
     flags = args.flags
     if args.workload == "chain" and not flags:
@@ -349,6 +354,32 @@ def main():
         for r in rows:
             print(json.dumps(r), file=sys.stderr)
     print(json.dumps(out))
+
+
+def feedforward(torch, wl, args):
+    """Blocks of pruned linear layers: a step is one pass of every block, a batch of tokens each; time of each library call."""
+    from paper_1802_10280_amd.runner import FeedForwardRunner
+    stream = torch.cuda.current_stream()
+    runners = [FeedForwardRunner(wl.make_block(n)) for n in wl.CONFIG_BLOCKS[args.workload]]
+    nnz = [len(r.block.up[1]) + len(r.block.down[1]) for r in runners]
+    flops = [2.0 * n * r.block.spec.T for n, r in zip(nnz, runners)]
+    sec = wall_time(torch, runners, args.steps, args.warmup)
+    med = np.median(time_kernels(torch, runners, max(20, min(args.steps, 100)), stream), axis=0)
+    rows, i = [], 0
+    for r, n, fl in zip(runners, nnz, flops):
+        s, names = r.block.spec, r.kernel_names()
+        t = {nm: round(float(med[i + j]) * 1e3, 2) for j, nm in enumerate(names)}
+        i += len(names)
+        # the kept weights and a bit for every place
+        weight_bytes = n * (4 if s.type == "f32" else 2) + 3 * s.D * s.F / 8
+        rows.append({"block": s.name, "tokens": s.T, "D": s.D, "F": s.F, "nnz": n, "us": t,
+                     "gflops": round(fl / sum(t.values()) / 1e3, 1), "weight_gbps": round(weight_bytes / sum(t.values()) / 1e3, 1)})
+    s = runners[0].block.spec
+    return {"metric": "effective GFLOP/s (2*nnz MACs a token) of pruned feed-forward blocks, norms included", "value": round(sum(flops) / sec / 1e9, 1),
+            "unit": "GFLOP/s", "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": round(sec * 1e3, 4), "higher_is_better": True,
+            "scaling": "weak", "vs_baseline": None, "dtype": s.type, "data": "synthetic",
+            "config": {"workload": f"{args.workload}: " + ",".join(r.block.spec.name for r in runners), "tokens": [r.block.spec.T for r in runners],
+                       "sparsity": s.sparsity, "cache_state": "warm (Infinity Cache)"}, "blocks": rows}
 
 
 def cpu_baseline(layers, images):

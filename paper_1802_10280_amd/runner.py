@@ -1,6 +1,7 @@
 """Per-layer driver used by the bench, the smoke check and the tests: packs the CSR once,
 uploads it, owns the torch device buffers and issues the library calls of one forward pass.
-It only marshals arguments; every step of the path runs inside libescoin.so."""
+It only marshals arguments; every step of the path runs inside libescoin.so.
+FeedForwardRunner does the same for a feed-forward block of pruned linear layers."""
 from __future__ import annotations
 
 import numpy as np
@@ -82,3 +83,55 @@ class LayerRunner:
         for k in self.kernels():
             k()
         return self.d_out
+
+
+TYPES = {"f32": B.T_F32, "f16": B.T_F16, "bf16": B.T_BF16}
+
+
+class FeedForwardRunner:
+    """One pruned feed-forward block: n = norm(x); g = silu(n Wg) * (n Wu); d = g Wd; h = x + gate * norm(d); and the next
+    block's n = norm(h)."""
+
+    def __init__(self, block, stream=None, before=None, eps: float = 1e-5):
+        """before: the runner of the block before this one, whose h and n this one reads (they need no norm of their own)."""
+        import torch
+        self.block, self.stream, self.before = block, stream, before
+        s = block.spec
+        type, dt = TYPES[s.type], (torch.float32, torch.float16, torch.bfloat16)[TYPES[s.type]]
+        up = lambda a: torch.from_numpy(np.ascontiguousarray(a)).to("cuda").to(dt)
+        new = lambda width: torch.empty((s.T, width), dtype=dt, device="cuda")
+        self.d_x, self.d_n = (before.d_h, before.d_next) if before is not None else (up(block.x), new(s.D))
+        assert tuple(self.d_x.shape) == (s.T, s.D) and self.d_x.dtype == dt
+        self.d_g, self.d_d, self.d_h, self.d_next = new(s.F), new(s.D), new(s.D), new(s.D)
+        self.d_norm, self.d_post, self.d_pre, self.d_gate = (up(a) for a in (block.norm, block.post_norm, block.next_norm, block.gate))
+        self.up_desc, self.down_desc = B.make_linear_desc(s.T, s.D, s.F, type, gated=True), B.make_linear_desc(s.T, s.F, s.D, type)
+        self.up_plan = B.escoin_linear_plan_build(self.up_desc, *block.up)
+        self.down_plan = B.escoin_linear_plan_build(self.down_desc, *block.down)
+        self.d_up, self.d_down = (torch.from_numpy(p).to("cuda") for p in (self.up_plan, self.down_plan))
+        self.first_desc = B.make_norm_desc(s.T, s.D, type, B.NORM_NONE, B.NORM_RMS, eps=eps)
+        self.last_desc = B.make_norm_desc(s.T, s.D, type, B.NORM_RMS, B.NORM_RMS, eps=eps)
+
+    def norm(self):
+        B.escoin_norm_forward(self.first_desc, self.d_x, None, self.d_n, d_pre_weight=self.d_norm, stream=self.stream)
+
+    def up(self):
+        B.escoin_linear_forward(self.up_desc, self.up_plan, self.d_up, self.d_n, self.d_g, flags=B.F_SILU, stream=self.stream)
+
+    def down(self):
+        B.escoin_linear_forward(self.down_desc, self.down_plan, self.d_down, self.d_g, self.d_d, stream=self.stream)
+
+    def sum(self):
+        B.escoin_norm_forward(self.last_desc, self.d_x, self.d_h, self.d_next, d_y=self.d_d, d_gate=self.d_gate,
+                              d_post_weight=self.d_post, d_pre_weight=self.d_pre, stream=self.stream)
+
+    def kernels(self):
+        """The library calls of one forward pass, in order."""
+        return [*([self.norm] if self.before is None else []), self.up, self.down, self.sum]
+
+    def kernel_names(self):
+        return [k.__name__ for k in self.kernels()]
+
+    def run(self):
+        for k in self.kernels():
+            k()
+        return self.d_h, self.d_next

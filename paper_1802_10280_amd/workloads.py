@@ -218,3 +218,56 @@ def custom_layer(N, C, H, W, M, R, S, stride, pad, sparsity, seed, dist="uniform
     rowptr, colidx, value = dense_to_csr(w)
     bias = rng.normal(0.0, 0.1, size=M).astype(np.float32)
     return Layer(spec, w, rowptr, colidx, value, make_input(spec, rng), bias)
+
+
+# ---- pruned feed-forward blocks (token-major activations) ----------------------------------------------------------------
+
+
+@dataclass(frozen=True)
+class BlockSpec:
+    """One feed-forward block: norm, gated product D -> F, product F -> D, norm of its output, gate, sum, next block's norm."""
+
+    name: str
+    T: int               # tokens
+    D: int               # features of the residual stream
+    F: int               # features inside the block
+    type: str            # "f32", "f16" or "bf16"
+    sparsity: float
+    seed: int = BASE_SEED + 900
+
+
+BLOCKS = {s.name: s for s in [
+    BlockSpec("F1", 1, 2048, 5632, "bf16", 0.60),          # one token of one user
+    BlockSpec("F32", 32, 2048, 5632, "bf16", 0.60),        # a serving batch
+    BlockSpec("F2048", 2048, 2048, 5632, "bf16", 0.60),    # a prompt
+]}
+CONFIG_BLOCKS = {"feedforward": ["F1", "F32", "F2048"]}
+
+
+@dataclass
+class Block:
+    """Values in fp32, as a checkpoint's; CSRs of 2F x D (the gates' rows first) and D x F."""
+
+    spec: BlockSpec
+    up: tuple                     # rowptr, colidx, value
+    down: tuple
+    norm: np.ndarray              # (D,) weight of the norm before the block
+    post_norm: np.ndarray         # ... of its output
+    next_norm: np.ndarray         # ... before the next block
+    gate: np.ndarray              # (D,) gate of the block's output
+    x: np.ndarray                 # (T, D) residual stream
+
+
+def make_block(spec: BlockSpec | str) -> Block:
+    if isinstance(spec, str):
+        spec = BLOCKS[spec]
+    rng = np.random.Generator(np.random.PCG64(spec.seed))
+
+    def csr(rows, cols):
+        w = rng.standard_normal((rows, cols), dtype=np.float32) * np.float32(1.0 / np.sqrt(max(1.0, cols * (1.0 - spec.sparsity))))
+        w[rng.random((rows, cols), dtype=np.float32) < spec.sparsity] = 0.0
+        return dense_to_csr(w)
+
+    vec = lambda shift: (rng.standard_normal(spec.D) * 0.1 + shift).astype(np.float32)
+    return Block(spec, csr(2 * spec.F, spec.D), csr(spec.D, spec.F), vec(1.0), vec(1.0), vec(1.0), vec(0.8),
+                 rng.standard_normal((spec.T, spec.D)).astype(np.float32) * np.float32(2.0))

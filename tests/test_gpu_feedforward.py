@@ -1,0 +1,99 @@
+"""Feed-forward blocks as they are used: the norms and the pruned layers after each other, each held to its definition in 64 bits
+on what the step before it handed over; blocks behind blocks, graphs of a whole block, two graphs at once."""
+import numpy as np
+import pytest
+
+import paper_1802_10280_amd as esc
+import feedforward as ff
+from paper_1802_10280_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": 0, "f16": 1, "bf16": 2}
+
+
+def dense(csr, rows, cols, type):
+    rowptr, colidx, value = csr
+    w = np.zeros((rows, cols))
+    w[np.repeat(np.arange(rows), np.diff(rowptr)), colidx] = ff.rounded(value, type)
+    return w
+
+
+def check(runner):
+    s, type = runner.block.spec, TYPES[runner.block.spec.type]
+    host = lambda t: t.double().cpu().numpy()
+    eps = float(np.float32(1e-5))
+    x, n, g, d, h, nxt = (host(t) for t in (runner.d_x, runner.d_n, runner.d_g, runner.d_d, runner.d_h, runner.d_next))
+    b = runner.block
+    if runner.before is None:
+        _, (ref, limit) = ff.block64(x, None, None, type, 0, 1, eps, 1.0, 1.0, 0.0, None, None, ff.rounded(b.norm, type), None)
+        ff.within(n, ref, limit, "norm")
+    ff.within(g, *ff.linear64(n, dense(b.up, 2 * s.F, s.D, type), type, ff.SILU, True), "up")
+    ff.within(d, *ff.linear64(g, dense(b.down, s.D, s.F, type), type, 0, False), "down")
+    (ref, limit), (ref2, limit2) = ff.block64(x, d, ff.rounded(b.gate, type), type, 1, 1, eps, 1.0, 1.0, 0.0, ff.rounded(b.post_norm, type), None,
+                                              ff.rounded(b.next_norm, type), None)
+    ff.within(h, ref, limit, "h")
+    ff.within(nxt, ref2, limit2, "next")
+
+
+@pytest.mark.parametrize("type", list(TYPES))
+@pytest.mark.parametrize("T,D,F", [(1, 96, 200), (2, 333, 129), (17, 512, 300), (64, 1000, 77), (200, 264, 520), (1, 1, 1)])
+def test_a_block(type, T, D, F):
+    from paper_1802_10280_amd.runner import FeedForwardRunner
+    r = FeedForwardRunner(wl.make_block(wl.BlockSpec("t", T, D, F, type, 0.6, seed=T + D)))
+    r.run()
+    check(r)
+
+
+@pytest.mark.parametrize("T", [1, 40, 150])
+def test_blocks_behind_each_other(T):
+    from paper_1802_10280_amd.runner import FeedForwardRunner
+    runners = []
+    for k in range(3):
+        block = wl.make_block(wl.BlockSpec("t", T, 320, 448, "bf16", 0.7, seed=20 + k))
+        runners.append(FeedForwardRunner(block, before=runners[-1] if k else None))
+    assert runners[1].kernel_names() == ["up", "down", "sum"]
+    for r in runners:
+        r.run()
+    for r in runners:
+        check(r)
+
+
+@pytest.mark.parametrize("T", [1, 33, 300])
+def test_graphs_of_whole_blocks(T):
+    """Two blocks captured apart and replayed on two streams at once, with eager calls of the same kernels between."""
+    import torch
+    from paper_1802_10280_amd.runner import FeedForwardRunner
+    runners = [FeedForwardRunner(wl.make_block(wl.BlockSpec("t", T, 256, 512, "f16", 0.5, seed=40 + k))) for k in range(2)]
+    want, graphs, streams = [], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for r in runners:
+        r.run()
+        want.append([t.clone() for t in (r.d_h, r.d_next)])
+    torch.cuda.synchronize()
+    for r, s in zip(runners, streams):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            r.run()
+        graphs.append(g)
+    for k in range(4):
+        for r in runners:
+            r.d_h.fill_(float(k))
+            r.d_next.zero_()
+            r.d_g.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for r, w in zip(runners, want):
+            assert (r.d_h == w[0]).all() and (r.d_next == w[1]).all()
+        runners[k % 2].run()
+        assert runners[k % 2].d_next.float().sum().isfinite()
+
+
+def test_bundled_blocks():
+    """The blocks that the bench times, checked like any other."""
+    from paper_1802_10280_amd.runner import FeedForwardRunner
+    for name in wl.CONFIG_BLOCKS["feedforward"][:2]:
+        r = FeedForwardRunner(wl.make_block(name))
+        r.run()
+        check(r)

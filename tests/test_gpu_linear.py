@@ -265,3 +265,24 @@ def test_binding_refuses_what_does_not_fit():
         kw.update(bad)
         with pytest.raises(TypeError):
             esc.escoin_linear_forward(d, **kw)
+
+
+# The tiles of the kernel for many tokens, which goes by how they fill 256 compute units: 64 by 32, 64 by 64, one of 128 by 128 a
+# unit, two, 256 by 256; a last step, row block and token block that are not whole.
+@gpu
+@pytest.mark.parametrize("type,K,M,T,gated", [
+    (2, 200, 300, 300, False), (2, 200, 1020, 500, False), (2, 200, 4090, 1000, False), (2, 264, 4090, 2041, False), (1, 136, 8180, 2041, False),
+    (2, 328, 4090, 2041, True), (1, 72, 2040, 1000, True), (2, 201, 4090, 1000, False), (1, 203, 2050, 300, True), (0, 100, 1500, 100, False),
+    (0, 100, 2000, 500, False), (0, 100, 2040, 2041, False), (0, 101, 2040, 2041, False), (0, 68, 1020, 2041, True)])
+def test_every_tile(type, K, M, T, gated):
+    layer = Layer(K, M, type, gated)
+    layer.check(T, BIAS | RESIDUAL | SILU)
+
+
+@gpu
+@pytest.mark.parametrize("type,K", [(2, 140001), (1, 140008), (0, 70003), (0, 70004)])
+def test_long_rows(type, K):
+    """More tiles to a wave than it has lanes to keep their starts in."""
+    layer = Layer(K, 5, type, sparsity=0.97)
+    for T in (1, 6, 20, 300):
+        layer.check(T, 0)
