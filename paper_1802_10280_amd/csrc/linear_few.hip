@@ -218,6 +218,7 @@ __global__ __launch_bounds__(64 * few_waves(TYPE, NT)) void linear_few_kernel(co
         tile(i, 0);
         tile(i + 1, 1);
     }
+    __builtin_amdgcn_s_waitcnt(0);  // the last copies to LDS, of nothing, do not meet the sums
     __syncthreads();
     f4* const parts = (f4*)(lds + 128);
 #pragma unroll
@@ -236,7 +237,7 @@ int launch_one(const LinearArgs& a, hipStream_t stream) {
     constexpr int waves_at_most = few_waves(TYPE, NT);
     int waves = waves_at_most;
     constexpr int kWave = std::max(few_buffer(TYPE, IN, NT, CHUNKS), NT * 1024);
-    while (waves * kWave + 128 > 160 * 1024) waves /= 2;
+    waves = std::min(waves, (160 * 1024 - 128) / kWave);
     // fewer waves of more tiles each once they fill the compute units (the registers are for 12 or 20 on each)
     while (waves > 4 && (int64_t)grid.x * grid.y * waves > 256 * (waves_at_most == 8 ? 12 : 20)) waves /= 2;
     waves = std::min(waves, a.col_tiles);

@@ -214,9 +214,13 @@ int launch_tile(const LinearArgs& a, hipStream_t stream) {
     } else {
         // one tile of 128 by 128 to a compute unit, four steps on their way; or two, a step each
         const int64_t n128 = tiles(128, 128);
-        const double t32 = 0.15 * rounds(tiles(64, 32), 256), t64 = 0.22 * rounds(tiles(64, 64), 256), t128 = n128 <= 256 ? 0.46 : WIDE ? 0.95 * rounds(n128, 512) : 0.46 * rounds(n128, 256);
-        if constexpr (WIDE)
-            if (1.6 * rounds(tiles(256, 256), 256) < std::min(std::min(t32, t64), t128)) return launch_one<TYPE, GATED, WIDE, 256, 256, 2, 4, 1, 2>(a, stream);
+        const double t32 = 0.15 * rounds(tiles(64, 32), 256), t64 = 0.22 * rounds(tiles(64, 64), 256), small = std::min(t32, t64);
+        const double t128 = n128 <= 256 ? 0.46 : WIDE ? 1.05 * rounds(n128, 512) : 0.46 * rounds(n128, 256);
+        if constexpr (WIDE) {
+            const double tall = 0.97 * rounds(tiles(256, 128), 256), large = 1.6 * rounds(tiles(256, 256), 256);
+            if (large < std::min(std::min(small, t128), tall)) return launch_one<TYPE, GATED, WIDE, 256, 256, 2, 4, 1, 2>(a, stream);
+            if (tall < std::min(small, t128)) return launch_one<TYPE, GATED, WIDE, 256, 128, 2, 2, 2, 3>(a, stream);
+        }
         if (t32 < std::min(t64, t128)) return launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, stream);
         if (t64 < t128) return launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, stream);
         if constexpr (WIDE)

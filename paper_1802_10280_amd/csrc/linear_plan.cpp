@@ -2,8 +2,10 @@
 #include <limits.h>
 #include <string.h>
 
+#include <atomic>
 #include <memory>
 #include <new>
+#include <thread>
 
 #include "linear.h"
 
@@ -96,30 +98,52 @@ inline uint16_t rounded<uint16_t>(float f, int type) { return type == ESCOIN_T_B
 inline bool is_zero(float v) { return v == 0.0f; }
 inline bool is_zero(uint16_t v) { return (v & 0x7fff) == 0; }
 
-// Fills the sections from 32 rows at a time, which are laid out with their zeros first.
+// Blocks of 32 rows that are filled one after the other; such runs of blocks are filled side by side.  A run's values start where they
+// would if every one before it took its 15 bytes of padding a tile, so that a plan does not depend on how many threads fill it.
+constexpr int kRunFrags = 64;
+constexpr int kMostThreads = 8;
+
+uint64_t run_start(const LinearDims& d, const int32_t* rowptr, int frag) {
+    const int rows = std::min(frag * kFragRows, d.rows());
+    const int64_t before = d.gated ? (int64_t)rowptr[rows / 2] + rowptr[d.M + rows / 2] - rowptr[d.M] : rowptr[rows];
+    const int tiles = std::min(frag * (kFragRows / kTileRows), d.row_tiles());
+    return ((uint64_t)before * d.size() + (uint64_t)tiles * d.col_tiles() * 15) / 16 * 16;
+}
+
+// From the first of a run's blocks on; which are laid out with their zeros first.  Returns the words of the fullest lane, or -1 without memory.
 template <typename V>
-int fill(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, const float* value, LinearHeader* h, char* plan) {
+int fill(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, const float* value, const LinearHeader& h, char* plan, int from_frag) {
     const int cols = std::max(d.col_tiles() * kTileCols, d.col_frags() * 32 / (int)sizeof(V));
     std::unique_ptr<float[]> sums(new (std::nothrow) float[cols]);
     std::unique_ptr<V[]> dense(new (std::nothrow) V[(size_t)kFragRows * cols]);
-    if (!sums || !dense) return ESCOIN_ESIZE;
+    if (!sums || !dense) return -1;
     std::fill_n(sums.get(), cols, 0.0f);
-    uint32_t* const mask = (uint32_t*)(plan + h->off_mask);
-    uint32_t* const start = (uint32_t*)(plan + h->off_start);
-    char* const kept = plan + h->off_kept;
-    const bool whole = d.T > h->few_tokens;
-    uint64_t at = 0;
+    uint32_t* const mask = (uint32_t*)(plan + h.off_mask);
+    uint32_t* const start = (uint32_t*)(plan + h.off_start);
+    char* const kept = plan + h.off_kept;
+    const bool whole = d.T > h.few_tokens;
+    const int to_frag = std::min(from_frag + kRunFrags, d.row_frags());
+    uint64_t at = run_start(d, rowptr, from_frag);
+    const uint64_t stop = to_frag == d.row_frags() ? h.off_whole - h.off_kept : run_start(d, rowptr, to_frag);
     int most = 0;
-    for (int rf = 0; rf < d.row_frags(); ++rf) {
+    for (int rf = from_frag; rf < to_frag; ++rf) {
         std::fill_n(dense.get(), (size_t)kFragRows * cols, V{});
         for (int i = 0; i < kFragRows; ++i) {
             const int r = rf * kFragRows + i;
             if (r >= d.rows()) break;
             const int m = d.gated ? (r >> 1) + (r & 1) * d.M : r;
-            // repeated columns are added up before the sum is rounded
-            for (int32_t j = rowptr[m]; j < rowptr[m + 1]; ++j) sums[colidx[j]] += value[j];
-            for (int32_t j = rowptr[m]; j < rowptr[m + 1]; ++j) dense[(size_t)i * cols + colidx[j]] = rounded<V>(sums[colidx[j]], d.type);
-            for (int32_t j = rowptr[m]; j < rowptr[m + 1]; ++j) sums[colidx[j]] = 0.0f;
+            const int32_t begin = rowptr[m], end = rowptr[m + 1];
+            V* const row = dense.get() + (size_t)i * cols;
+            bool ascending = true;
+            for (int32_t j = begin + 1; j < end; ++j) ascending &= colidx[j] > colidx[j - 1];
+            if (ascending) {
+                for (int32_t j = begin; j < end; ++j) row[colidx[j]] = rounded<V>(value[j], d.type);
+            } else {
+                // repeated columns are added up before the sum is rounded
+                for (int32_t j = begin; j < end; ++j) sums[colidx[j]] += value[j];
+                for (int32_t j = begin; j < end; ++j) row[colidx[j]] = rounded<V>(sums[colidx[j]], d.type);
+                for (int32_t j = begin; j < end; ++j) sums[colidx[j]] = 0.0f;
+            }
         }
         for (int half = 0; half < kFragRows / kTileRows; ++half) {
             const int rt = rf * (kFragRows / kTileRows) + half;
@@ -130,15 +154,17 @@ int fill(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, cons
                 for (int lane = 0; lane < 64; ++lane) {
                     const V* const from = dense.get() + (size_t)(half * kTileRows + lane % 16) * cols + ct * kTileCols + lane / 16 * 8;
                     uint32_t bits = 0;
-                    V* const to = (V*)(kept + at);
+                    V found[33];
                     int n = 0;
                     for (int b = 0; b < 4; ++b)
                         for (int j = 0; j < 8; ++j) {
                             const V v = from[b * 32 + j];
-                            if (is_zero(v)) continue;
-                            bits |= 1u << (b * 8 + j);
-                            to[n++] = v;
+                            const uint32_t there = !is_zero(v);  // no branch: every other one would be guessed wrong
+                            found[n] = v;
+                            n += there;
+                            bits |= there << (b * 8 + j);
                         }
+                    memcpy(kept + at, found, n * sizeof(V));
                     most = std::max(most, (int)((at % 4 + n * sizeof(V) + 3) / 4));
                     at += n * sizeof(V);
                     mask[tile * 64 + lane] = bits;
@@ -147,16 +173,40 @@ int fill(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, cons
             }
         }
         if (!whole) continue;
-        char* to = plan + h->off_whole + (size_t)rf * d.col_frags() * kFragBytes;
+        char* to = plan + h.off_whole + (size_t)rf * d.col_frags() * kFragBytes;
         constexpr int kHalf = 16 / sizeof(V);  // columns of a lane
         for (int cf = 0; cf < d.col_frags(); ++cf)
             for (int lane = 0; lane < 64; ++lane, to += 16)
                 memcpy(to, dense.get() + (size_t)(lane % 32) * cols + (cf * 2 + lane / 32) * kHalf, 16);
     }
-    start[(size_t)d.row_tiles() * d.col_tiles()] = (uint32_t)(at / 16);
-    memset(kept + at, 0, (size_t)(h->off_whole - h->off_kept - at));
-    h->most_lane_words = most;
-    return ESCOIN_OK;
+    memset(kept + at, 0, (size_t)(stop - at));
+    if (to_frag == d.row_frags()) start[(size_t)d.row_tiles() * d.col_tiles()] = (uint32_t)(at / 16);
+    return most;
+}
+
+// All runs, by as many threads as there are runs (and as the machine gives: at least this one).
+template <typename V>
+int fill_all(const LinearDims& d, const int32_t* rowptr, const int32_t* colidx, const float* value, LinearHeader* h, char* plan) {
+    const int runs = (d.row_frags() + kRunFrags - 1) / kRunFrags;
+    std::atomic<int> next{0}, most{0};
+    const auto work = [&]() {
+        for (int r; (r = next.fetch_add(1)) < runs;) {
+            const int words = fill<V>(d, rowptr, colidx, value, *h, plan, r * kRunFrags);
+            int seen = most.load();
+            while (seen >= 0 && (words < 0 || words > seen) && !most.compare_exchange_weak(seen, words)) {}
+        }
+    };
+    std::thread others[kMostThreads - 1];
+    int started = 0;
+    const int wanted = std::min(std::min(runs, kMostThreads), (int)std::max(1u, std::thread::hardware_concurrency())) - 1;
+    try {
+        for (; started < wanted; ++started) others[started] = std::thread(work);
+    } catch (...) {
+    }
+    work();
+    for (int i = 0; i < started; ++i) others[i].join();
+    h->most_lane_words = most.load();
+    return most.load() < 0 ? ESCOIN_ESIZE : ESCOIN_OK;
 }
 
 }  // namespace
@@ -216,7 +266,8 @@ int escoin_linear_plan_build(const escoin_linear_desc* desc, const int32_t* rowp
     LinearHeader h = layout(d, rowptr[d.rows()]);
     if (plan_bytes < h.total_bytes) return ESCOIN_ESIZE;
     memset(plan, 0, (size_t)h.off_mask);
-    rc = d.type == ESCOIN_T_F32 ? fill<float>(d, rowptr, colidx, value, &h, (char*)plan) : fill<uint16_t>(d, rowptr, colidx, value, &h, (char*)plan);
+    memset((char*)plan + h.off_kept - 256, 0, 256);  // what lies between the tables and the values; the table's end is written below
+    rc = d.type == ESCOIN_T_F32 ? fill_all<float>(d, rowptr, colidx, value, &h, (char*)plan) : fill_all<uint16_t>(d, rowptr, colidx, value, &h, (char*)plan);
     if (rc == ESCOIN_OK) memcpy(plan, &h, sizeof(h));
     return rc;
 }

@@ -239,6 +239,26 @@ def test_graphs_and_streams(type, T):
 
 
 @gpu
+@pytest.mark.parametrize("K,M,T", [(1024, 2048, 64), (256, 4096, 1000), (256, 4096, 2048), (256, 8192, 2048)])
+def test_graphs_of_kernels_with_much_lds(K, M, T):
+    import torch
+    layer = Layer(K, M, 2, sparsity=0.3)
+    x = ff.to_dev(layer.inputs(T)[0], 2)
+    out = torch.empty((T, M), dtype=torch.bfloat16, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer.forward(x, RELU, out=out)
+    eager = layer.forward(x, RELU)
+    for k in range(3):
+        out.fill_(-1.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (out == eager).all()
+        assert layer.forward(x, 0).isfinite().all()
+
+
+@gpu
 def test_one_plan_for_calls_of_every_length():
     layer = Layer(640, 80, 2)
     for T in (300, 1, 64, 65, 17, 2):
