@@ -64,6 +64,9 @@ def test_kinds_and_gates(type, post, pre, gate):
 def test_tokens(type, T):
     check(T, 200, type)
     check(T, 131, type, 2, 2)
+    if T >= 1000:
+        check(T, 1003, type)
+        check(T, 4091, type, 1, 2)
 
 
 @gpu
