@@ -5,7 +5,6 @@
 namespace escoin {
 namespace {
 
-constexpr int kStep = kStepFrags * 32;  // bytes of a row to a step
 constexpr int kXcds = 8, kGroup = 8;
 
 // The tile of a workgroup.  Workgroups go to the XCDs in turn; each XCD gets tiles that follow one another, and those that run
@@ -24,21 +23,23 @@ constexpr int many_pitch(int fragments) { return fragments * 128 + 16; }  // byt
 // token by token, the 16-byte pieces of a token's 128 bytes turned about by its number so that 16 lanes' reads meet all banks.
 // Two steps are in LDS: while one is multiplied, the next one comes.  A wave reads its next fragments while it multiplies; the
 // last of a step are in registers when the waves meet, so that what follows the meeting has work to hide behind.
-template <int TYPE, bool GATED, bool WIDE, int BM, int BN, int WM, int WN, int WK, int NS>
+template <int TYPE, bool GATED, bool WIDE, int BM, int BN, int WM, int WN, int WK, int NS, int SF = kStepFrags>
 __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const LinearArgs a, int n_row_tiles, int n_token_tiles) {
     extern __shared__ char lds[];
     constexpr int kWaves = WM * WN * WK, kThreads = 64 * kWaves, kFM = BM / 32 / WM, kFN = BN / 32 / WN;  // fragments of a wave
+    constexpr int kStep = SF * 32, kTokenPieces = SF * 2;  // bytes of a row to a step, pieces of 16 of them
     constexpr int kWeightBytes = BM * kStep, kBuffer = (BM + BN) * kStep;
-    constexpr int kSize = sizeof(typename Num<TYPE>::type), kPieces = BN * 8 / kThreads, kFrags = BM / 32 * kStepFrags / kWaves;
+    constexpr int kSize = sizeof(typename Num<TYPE>::type), kPieces = BN * kTokenPieces / kThreads, kFrags = BM / 32 * SF / kWaves;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int row_tile, token_tile;
     place(n_row_tiles, n_token_tiles, &row_tile, &token_tile);
-    const int row0 = row_tile * BM, token0 = token_tile * BN, end = a.K * kSize, steps = a.col_frags / kStepFrags;
+    const int row0 = row_tile * BM, token0 = token_tile * BN, end = a.K * kSize, steps = (a.col_frags + SF - 1) / SF;
 
     // What a thread copies: of the weights 16 bytes of the wave's share of the fragments, of the inputs a piece of every kThreads / 8
     // tokens, by way of buffers: 32-bit offsets leave the registers to the sums, and the compiler waits for every LDS read
     // as long as a copy to LDS by a global address is on its way.
-    const int piece = (tid & 7) ^ (tid >> 4 & 7);
+    const auto turned = [](int token) { return SF == 4 ? token >> 1 & 7 : token & 15; };
+    const int my_token = tid / kTokenPieces, piece = tid % kTokenPieces ^ turned(my_token);
     const char* const x_base = a.in + token0 * a.ld_in;
     const Buffer w_buffer = buffer(a.whole + (size_t)(row0 / kFragRows) * a.col_frags * kFragBytes, 0xffffffffu), x_buffer = buffer(x_base, 0xffffffffu);
     const int frag_rows = a.row_frags - row0 / kFragRows;  // from the tile's first on
@@ -46,7 +47,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
     const char* x_row[WIDE ? 1 : kPieces];
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-        const int token = min(p * (kThreads / 8) + (tid >> 3), a.T - 1 - token0);
+        const int token = min(p * (kThreads / kTokenPieces) + my_token, a.T - 1 - token0);
         if constexpr (WIDE) x_off[p] = (uint32_t)token * (uint32_t)a.ld_in + piece * 16;
         else x_row[p] = x_base + token * a.ld_in;
     }
@@ -58,8 +59,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
     const auto ask = [&](int step, char* to) {
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) {
-            const int i = f * kWaves + wave, frag = min(i / kStepFrags, frag_rows - 1);
-            copy16(w_buffer, lane * 16, (frag * a.col_frags + step * kStepFrags + i % kStepFrags) * kFragBytes, to + i * kFragBytes);
+            const int i = f * kWaves + wave, frag = min(i / SF, frag_rows - 1), col = step * SF + i % SF;
+            copy16(w_buffer, lane * 16, (frag * a.col_frags + (SF == kStepFrags ? col : min(col, a.col_frags - 1))) * kFragBytes, to + i * kFragBytes);
         }
         if constexpr (WIDE) {
             char* const x_to = to + kWeightBytes + wave * 1024;
@@ -82,16 +83,17 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
 
     f16v sum[kFM][kFN] = {};
     const int wk = wave / (WM * WN), wm = wave / WN % WM, wn = wave % WN;
-    const int turn = lane >> 1 & 7, q = lane >> 5, w_at = (wm * kFM * kStepFrags + wk) * kFragBytes + lane * 16;
+    const int turn = turned(lane & 31), q = lane >> 5, w_at = (wm * kFM * SF + wk) * kFragBytes + lane * 16;
     const int x_at = kWeightBytes + (wn * kFN * 32 + lane % 32) * kStep;
     u4 w[2][kFM], x[2][kFN];
     const auto read = [&](const char* from, int k, int to) {
 #pragma unroll
         for (int n = 0; n < kFN; ++n) x[to][n] = *(const u4*)(from + x_at + n * 32 * kStep + ((((k * WK + wk) * 2 + q) ^ turn) * 16));
 #pragma unroll
-        for (int m = 0; m < kFM; ++m) w[to][m] = *(const u4*)(from + w_at + (m * kStepFrags + k * WK) * kFragBytes);
+        for (int m = 0; m < kFM; ++m) w[to][m] = *(const u4*)(from + w_at + (m * SF + k * WK) * kFragBytes);
     };
-    const auto multiply = [&](int from) {
+    const auto multiply = [&](int from, int frag) {
+        if (SF > kStepFrags && frag >= a.col_frags) return;  // steps of eight fragments where the last holds four
 #pragma unroll
         for (int m = 0; m < kFM; ++m)
 #pragma unroll
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
             put(lds + s * kBuffer);
         }
     arrived(steps < NS);
-    constexpr int kOwn = kStepFrags / WK;  // fragments of a step that are a wave's
+    constexpr int kOwn = SF / WK;  // fragments of a step that are a wave's
     int at = 0;                            // the step's place in the ring
     read(lds, 0, 0);
     for (int step = 0; step < steps; ++step) {
@@ -131,7 +133,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
         for (int k = 0; k < kOwn - 1; ++k) {
             read(now, k + 1, ~k & 1);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(k & 1);
+            multiply(k & 1, step * SF + k * WK + wk);
             __builtin_amdgcn_sched_barrier(0);
         }
         if (step + 1 < steps) {
@@ -139,7 +141,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
             if constexpr (kOwn > 1) read(lds + at * kBuffer, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        multiply((kOwn - 1) & 1);
+        multiply((kOwn - 1) & 1, step * SF + (kOwn - 1) * WK + wk);
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (kOwn == 1)
             if (step + 1 < steps) read(lds + at * kBuffer, 0, 0);
@@ -188,17 +190,17 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
     }
 }
 
-template <int TYPE, bool GATED, bool WIDE, int BM, int BN, int WM, int WN, int WK, int NS>
+template <int TYPE, bool GATED, bool WIDE, int BM, int BN, int WM, int WN, int WK, int NS, int SF = kStepFrags>
 int launch_one(const LinearArgs& a, hipStream_t stream) {
-    constexpr int kLds = std::max(NS * (BM + BN) * kStep, WM * WN * WK * 32 * many_pitch(BM / 32 / WM)), kThreads = 64 * WM * WN * WK;
+    constexpr int kLds = std::max(NS * (BM + BN) * SF * 32, WM * WN * WK * 32 * many_pitch(BM / 32 / WM)), kThreads = 64 * WM * WN * WK;
     const int64_t rows = (a.rows + BM - 1) / BM, tokens = ((int64_t)a.T + BN - 1) / BN;
     if (!grid_fits((double)rows * tokens, kThreads)) return ESCOIN_ERANGE;
-    const auto kernel = linear_many_kernel<TYPE, GATED, WIDE, BM, BN, WM, WN, WK, NS>;
+    const auto kernel = linear_many_kernel<TYPE, GATED, WIDE, BM, BN, WM, WN, WK, NS, SF>;
     const int rc = kLds > 64 * 1024 ? allow_dynamic_lds((const void*)kernel, kLds) : ESCOIN_OK;
     return rc != ESCOIN_OK ? rc : launch(kernel, dim3((unsigned)(rows * tokens)), dim3(kThreads), (size_t)kLds, stream, a, (int)rows, (int)tokens);
 }
 
-// Which tile: the one whose steps take the least time, by how many of its tiles the fullest compute unit gets.  Microseconds a step,
+// Which tile: the one whose steps take the least time, by how many of its tiles the fullest compute unit gets.  Microseconds a step of 128 bytes a row,
 // measured with 256 to 25000 rows and 64 to 4096 tokens: 16-bit types are bound by the copies to LDS with small tiles (a step of 64 by 64
 // brings 16 KB for 0.5 MFLOP, of 256 by 256 64 KB for 8), fp32 by the matrix cores with any, so that there the smallest come
 // first.  Inputs that come through registers have the tiles whose ring holds three steps or more.
@@ -207,22 +209,29 @@ int launch_tile(const LinearArgs& a, hipStream_t stream) {
     const auto tiles = [&](int rows, int tokens) { return ((int64_t)a.rows + rows - 1) / rows * (((int64_t)a.T + tokens - 1) / tokens); };
     const auto rounds = [](int64_t n, int units) { return (double)((n + units - 1) / units); };
     if constexpr (TYPE == ESCOIN_T_F32) {
-        const double t32 = 0.27 * rounds(tiles(64, 32), 256), t64 = 0.52 * rounds(tiles(64, 64), 256), t128 = 1.95 * rounds(tiles(128, 128), 256);
-        if (t32 < std::min(t64, t128)) return launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, stream);
+        const int64_t n32 = tiles(64, 32);
+        const double t32 = n32 <= 256 ? 0.24 : 0.255 * rounds(n32, 256), t64 = 0.52 * rounds(tiles(64, 64), 256), t128 = 1.95 * rounds(tiles(128, 128), 256);
+        // (two small tiles to a compute unit or fewer: twice the columns to a step, by more waves; 1001 to 1503, 250 tokens 16.7 us and 18.4)
+        if (t32 < std::min(t64, t128))
+            return n32 <= 512 ? launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 4, 3, 8>(a, stream) : launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, stream);
         if (t64 < t128) return launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, stream);
         return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, WIDE ? 2 : 4>(a, stream);
     } else {
         // one tile of 128 by 128 to a compute unit, four steps on their way; or two, a step each
         const int64_t n128 = tiles(128, 128);
-        const double t32 = 0.15 * rounds(tiles(64, 32), 256), t64 = 0.22 * rounds(tiles(64, 64), 256), small = std::min(t32, t64);
+        const int64_t n32 = tiles(64, 32), n64 = tiles(64, 64);
+        const double t32 = n32 <= 256 ? 0.135 : 0.15 * rounds(n32, 256), t64 = n64 <= 256 ? 0.185 : 0.22 * rounds(n64, 256), small = std::min(t32, t64);
         const double t128 = n128 <= 256 ? 0.46 : WIDE ? 1.05 * rounds(n128, 512) : 0.46 * rounds(n128, 256);
         if constexpr (WIDE) {
             const double tall = 0.97 * rounds(tiles(256, 128), 256), large = 1.6 * rounds(tiles(256, 256), 256);
             if (large < std::min(std::min(small, t128), tall)) return launch_one<TYPE, GATED, WIDE, 256, 256, 2, 4, 1, 2>(a, stream);
             if (tall < std::min(small, t128)) return launch_one<TYPE, GATED, WIDE, 256, 128, 2, 2, 2, 3>(a, stream);
         }
-        if (t32 < std::min(t64, t128)) return launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, stream);
-        if (t64 < t128) return launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, stream);
+        // (one small tile to a compute unit: half as many steps of twice the columns, by more waves; 2560 to 2560, 53 tokens 9.4 us and 10.3)
+        if (t32 < std::min(t64, t128))
+            return n32 <= 256 ? launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 4, 3, 8>(a, stream) : launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, stream);
+        if (t64 < t128)
+            return n64 <= 256 ? launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3, 8>(a, stream) : launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, stream);
         if constexpr (WIDE)
             if (n128 > 256) return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, 2>(a, stream);
         return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, 4>(a, stream);

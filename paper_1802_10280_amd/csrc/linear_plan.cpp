@@ -41,18 +41,19 @@ inline uint16_t fp16_bits(float f) {
 }
 
 // Up to how many tokens the kept weights are read.  Every workgroup unfolds them for itself, for 64 tokens at a time (fp32: 32): microseconds
-// a tile and compute unit.  The tiled kernel's time is its steps (linear_many.hip), but no less than the whole weights take from memory;
-// it needs rows enough to be spread over the compute units.  Measured with 64 tokens at 50 %, kept against whole: 12288 to 4096 34
-// and 53 us, 2560 to 2560 10.7 and 11, 4096 to 24576 73 and 34, at 32 tokens 37.7 and 32.1 (41 from memory).
+// a tile and compute unit, and two more to begin with than the tiled kernel where it is more than 32; inputs whose rows cannot all start on 16 bytes
+// cost more.  The tiled kernel's time is its steps (linear_many.hip), but no less than the whole weights take from memory; it
+// needs rows enough to be spread over the compute units.  Measured with 64 tokens at 50 %, kept against whole: 12288 to 4096 34
+// and 33 us, 12288 to 2048 21 and 32, 2560 to 2560 10.7 and 9.4, 4096 to 24576 73 and 34, at 32 tokens 37.7 and 32.1 (41 from memory).
 int few_tokens(const LinearDims& d) {
     const bool f32 = d.type == ESCOIN_T_F32;
     const double tiles = (double)d.row_tiles() * d.col_tiles() / 256, steps = d.col_frags() / kStepFrags;
-    const double memory = (double)d.row_frags() * d.col_frags() * kFragBytes / 4.9e6;
+    const double memory = (double)d.row_frags() * d.col_frags() * kFragBytes / 4.9e6, narrow = (int64_t)d.K * d.size() % 16 ? 1.3 : 1.0;
     int most = 16;
     for (int T = 32; T <= 256; T += 32) {
         const double kept = f32 ? 0.61 * (T / 32) : T <= 32 ? 0.18 : 0.30 * ((T + 63) / 64);
         const double rounds = (double)((((d.rows() + 63) / 64) * (int64_t)(T / 32) + 255) / 256);
-        if (kept * tiles <= std::max(memory, (f32 ? 0.27 : 0.155) * steps * rounds)) most = T;
+        if (kept * narrow * tiles + (T > 32 ? 2.0 : 1.0) <= std::max(memory, (f32 ? 0.24 : 0.135) * steps * rounds)) most = T;
     }
     return most;
 }
