@@ -212,6 +212,7 @@ int escoin_sconv_tiled_kernel(const escoin_conv_desc *desc, const void *plan_hos
  *     elements; 0: next to each other).  Every tensor of a call, parameters too, has the descriptor's type; pointers are
  *     aligned to it.  Sums and statistics are fp32, an output is rounded once (to nearest even).
  *   - T == 0 is a call that does nothing and returns ESCOIN_OK.  Rows from T on are neither read nor written.
+ *   - ESCOIN_ERANGE also where a launch would have 2^32 threads (some four million rows of a long norm).
  */
 enum { ESCOIN_T_F32 = 0, ESCOIN_T_F16 = 1, ESCOIN_T_BF16 = 2 };
 
@@ -244,7 +245,8 @@ int escoin_linear_check_desc(const escoin_linear_desc *desc);
  * built with is the most tokens that calls with it may have.
  *   rowptr, colidx, value  host CSR, columns of a row in any order; repeated ones are added up in fp32
  *   plan_size     an upper bound on the blob's size, from the descriptor and the number of nonzeros
- *   plan_build    fills it; ESCOIN_ESIZE if it is smaller than plan_size tells, ESCOIN_EINVAL on a malformed CSR
+ *   plan_build    fills it, by up to eight threads; equal calls give equal bytes.  ESCOIN_ESIZE if it is smaller than plan_size
+ *                 tells (or there is no memory for 32 rows a thread), ESCOIN_EINVAL on a malformed CSR
  * Both run on the host and need no GPU.
  */
 int escoin_linear_plan_size(const escoin_linear_desc *desc, const int32_t *rowptr, const int32_t *colidx, size_t *plan_bytes);
