@@ -259,7 +259,7 @@ class _Rows:
         if not _torch_types:
             import torch
             _torch_types.extend((torch.float32, torch.float16, torch.bfloat16))
-        self.type, self.device = _torch_types[type], -1
+        self.type, self.device = _torch_types[type], -2    # (a CPU tensor's is -1)
 
     def _seen(self, t):
         if t.dtype is not self.type:
@@ -276,7 +276,8 @@ class _Rows:
         """Pointer to T rows of `width` elements, `ld` (0: width) apart, or None."""
         if t is None:
             return None
-        self._seen(t)
+        if t.dtype is not self.type or t.get_device() != self.device:
+            self._seen(t)
         shape, stride = t.shape, t.stride()
         if len(shape) != 2 or shape[0] < T or shape[1] != width or (width > 1 and stride[1] != 1) or (T > 1 and stride[0] != (ld or width)):
             raise TypeError(f"expected {T} rows of {width}, {ld or width} elements apart: got shape {tuple(shape)}, strides {stride}")
@@ -285,7 +286,8 @@ class _Rows:
     def vector(self, t, width):
         if t is None:
             return None
-        self._seen(t)
+        if t.dtype is not self.type or t.get_device() != self.device:
+            self._seen(t)
         if t.numel() != width or not t.is_contiguous():
             raise TypeError(f"expected {width} contiguous elements: got shape {tuple(t.shape)}, strides {t.stride()}")
         return t.data_ptr()
@@ -293,7 +295,9 @@ class _Rows:
     def call(self, where, fn, *args, stream):
         """The library launches on the current device: the tensors' own for the time of the call."""
         import torch
-        if self.device != torch.cuda.current_device():
+        if self.device < 0:
+            raise TypeError("a call without tensors")
+        if self.device != torch._C._cuda_getDevice():  # (the runtime runs: there are tensors)
             with torch.cuda.device(self.device):
                 return _check(fn(*args, _stream(stream)), where)
         rc = fn(*args, torch._C._cuda_getCurrentRawStream(self.device) if stream is None else _stream(stream))
@@ -334,7 +338,7 @@ def escoin_linear_plan_build(desc, rowptr: np.ndarray, colidx: np.ndarray, value
 
 
 def escoin_linear_few_tokens(desc, plan_host: np.ndarray) -> int:
-    rc = lib().escoin_linear_few_tokens(ctypes.byref(desc), _plan_ptr(plan_host))
+    rc = lib().escoin_linear_few_tokens(ctypes.byref(desc), _plan_header(plan_host))
     if rc < 0:
         _check(rc, "escoin_linear_few_tokens")
     return rc
@@ -350,10 +354,11 @@ class _LinearHeader(ctypes.Structure):
 _BYTES, _HEADER_BYTES = np.dtype(np.uint8), ctypes.sizeof(_LinearHeader)
 
 
-def _plan_ptr(plan: np.ndarray):
-    if not isinstance(plan, np.ndarray) or plan.dtype != _BYTES or not plan.flags.c_contiguous or plan.nbytes < _HEADER_BYTES:
+def _plan_header(plan: np.ndarray) -> bytes:
+    """The bytes of the plan that a call reads on the host (a copy of them is had sooner than the array's address)."""
+    if not isinstance(plan, np.ndarray) or plan.dtype != _BYTES or plan.ndim != 1 or plan.strides[0] != 1 or plan.size < _HEADER_BYTES:
         raise TypeError("this is no plan of a linear layer")
-    return plan.__array_interface__["data"][0]
+    return plan[:_HEADER_BYTES].tobytes()
 
 
 def linear_plan_header(plan: np.ndarray) -> dict:
@@ -367,8 +372,8 @@ def escoin_linear_forward(desc, plan_host: np.ndarray, d_plan, d_in, d_out, d_bi
     T, rows = max(desc.T, 0), desc.M * (2 if desc.gated else 1)
     args = (t.rows(d_in, T, desc.K, desc.ld_in), t.rows(d_out, T, desc.M, desc.ld_out), t.vector(d_bias, rows),
             t.rows(d_residual, T, desc.M, desc.ld_residual))
-    plan = _plan_ptr(plan_host)
-    if d_plan.get_device() != t.device or d_plan.nbytes < plan_host.nbytes or not d_plan.is_contiguous():
+    plan = _plan_header(plan_host)
+    if d_plan.get_device() != t.device or d_plan.nbytes < plan_host.size or not d_plan.is_contiguous():
         raise TypeError("the plan's copy has to be whole and on the tensors' device")
     t.call("escoin_linear_forward", lib().escoin_linear_forward, ctypes.byref(desc), plan, d_plan.data_ptr(), *args, flags, stream=stream)
 

@@ -306,3 +306,12 @@ def test_long_rows(type, K):
     layer = Layer(K, 5, type, sparsity=0.97)
     for T in (1, 6, 20, 300):
         layer.check(T, 0)
+
+
+@gpu
+@pytest.mark.parametrize("type,K,M,T,gated", [(2, 12288, 1500, 100, False), (1, 12280, 750, 128, True), (0, 4096, 1024, 150, False), (0, 4097, 1000, 70, False)])
+def test_kept_weights_for_many_tokens(type, K, M, T, gated):
+    """Long rows, few of them: the kept weights are read for more tokens than a workgroup takes."""
+    layer = Layer(K, M, type, gated, sparsity=0.9)
+    assert layer.few >= T
+    layer.check(T, BIAS | RESIDUAL | GELU_TANH)

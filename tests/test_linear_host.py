@@ -237,6 +237,11 @@ class Tensor:
         return 4096
 
 
+def test_a_call_without_tensors_is_refused():
+    with pytest.raises(TypeError):
+        esc.escoin_norm_forward(esc.make_norm_desc(2, 8, esc.T_F32), None, None, None)
+
+
 class Reached(Exception):
     pass
 
@@ -279,6 +284,11 @@ def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
         esc.escoin_linear_forward(wide, **{**ok, "d_in": Tensor([T, K], stride=(K + 8, 1))})
     with pytest.raises(TypeError):
         esc.escoin_linear_forward(wide, **ok)
+
+    with pytest.raises(TypeError):
+        esc.escoin_linear_forward(d, plan, ok["d_plan"], None, None)
+    with pytest.raises(TypeError):
+        esc.escoin_linear_forward(d, plan, ok["d_plan"], Tensor([T, K], device=-1), Tensor([T, M], device=-1))
 
     D = 24
     for rows in (0, 1):
