@@ -19,6 +19,12 @@ typedef __amdgpu_buffer_rsrc_t Buffer;
 __device__ inline Buffer buffer(const char* p, uint32_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000); }
 __device__ inline u4 load16(Buffer from, int lane_offset, int offset) { return __builtin_amdgcn_raw_buffer_load_b128(from, lane_offset, offset, 0); }
 
+// What stands before it in the source is issued before it: a wait that counts the loads on their way goes by their order.
+__device__ inline void in_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // 16 bytes a lane: 1024 of LDS from `to` on
 __device__ inline void copy16(Buffer from, int lane_offset, int offset, char* to) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Lds)to, 16, lane_offset, offset, 0, 0);

@@ -168,7 +168,11 @@ __global__ __launch_bounds__(64 * few_waves(TYPE, NT)) void linear_few_kernel(co
 #pragma unroll
     for (int i = 0; i < 3; ++i) mask[i] = ask_mask(i);
     ask(0, mask[0], 0);
-    if constexpr (IN == kInLds) inputs(wave, true);
+    if constexpr (IN == kInLds) {
+        in_order();
+        inputs(wave, true);
+        in_order();
+    }
     ask(1, mask[1], 1);
     if constexpr (IN != kInLds) inputs(wave, true);
     __syncthreads();
@@ -182,9 +186,9 @@ __global__ __launch_bounds__(64 * few_waves(TYPE, NT)) void linear_few_kernel(co
             for (int j = 0; j < 4; ++j) at_lds<uint32_t>(column)[(c * 4 + j) * 64] = v[slot][c][j];
         if constexpr (IN == kInLds) {
             // the tile's inputs have come once no more is on its way than the next tile's values
-            asm volatile("" ::: "memory");
+            in_order();
             __builtin_amdgcn_s_waitcnt(0x0f70 | CHUNKS);
-            asm volatile("" ::: "memory");
+            in_order();
             const char* const mine = lds + 128 + wave * kBuffer + kColumns + lane % 16 * kRowBytes;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
@@ -193,10 +197,11 @@ __global__ __launch_bounds__(64 * few_waves(TYPE, NT)) void linear_few_kernel(co
 #pragma unroll
                     for (int p = 0; p < kParts; ++p)
                         x[b][t][p] = *(const u4*)(mine + t * 16 * kRowBytes + (((b * 4 + lane / 16) * kParts + p) ^ (lane & 15)) * 16);
-            asm volatile("" ::: "memory");
+            in_order();
             __builtin_amdgcn_s_waitcnt(0xc07f);  // read, before the next tile's take their place
-            asm volatile("" ::: "memory");
+            in_order();
             inputs(wave + (i + 1) * waves, i + 1 < tiles);
+            in_order();
         }
         mask[0] = mask[1], mask[1] = mask[2], mask[2] = ask_mask(i + 3);
         if ((i & 63) == 62) look(i + 2);

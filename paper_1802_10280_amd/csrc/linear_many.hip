@@ -20,8 +20,8 @@ __device__ inline void place(int n_rows, int n_tokens, int* row, int* token) {
 constexpr int many_pitch(int fragments) { return fragments * 128 + 16; }  // bytes of a token's fp32 sums in LDS
 
 // A workgroup's waves, WM by WN of them, share BM rows and BN tokens.  A step's weights lie in LDS fragment by fragment, its inputs
-// token by token, the 16-byte pieces of a token's 128 bytes turned about by its number so that 16 lanes' reads meet all banks.
-// Two steps are in LDS: while one is multiplied, the next one comes.  A wave reads its next fragments while it multiplies; the
+// token by token, the 16-byte pieces of a token's 128 bytes (SF = 8: 256) turned about by its number so that 16 lanes' reads meet all banks.
+// NS steps are in LDS in a ring: while one is multiplied, the next ones come.  WK waves share a tile's columns, fragment by fragment.  A wave reads its next fragments while it multiplies; the
 // last of a step are in registers when the waves meet, so that what follows the meeting has work to hide behind.
 template <int TYPE, bool GATED, bool WIDE, int BM, int BN, int WM, int WN, int WK, int NS, int SF = kStepFrags>
 __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const LinearArgs a, int n_row_tiles, int n_token_tiles) {
@@ -103,23 +103,22 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
     const auto arrived = [&](bool all) {
         constexpr int kLater = (NS - 2) * (kFrags + kPieces);
         static_assert(kLater < 64, "six bits count the loads on their way");
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
+        in_order();
         if (all || NS == 2) __builtin_amdgcn_s_waitcnt(0);
         else __builtin_amdgcn_s_waitcnt(0x0070 | (kLater & 15) | (kLater >> 4) << 14);  // and for all of LDS
         __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("" ::: "memory");
+        in_order();
     };
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s)
         if (s < steps) {
             ask(s, lds + s * kBuffer);
             put(lds + s * kBuffer);
+            in_order();
         }
     arrived(steps < NS);
     constexpr int kOwn = SF / WK;  // fragments of a step that are a wave's
-    int at = 0;                            // the step's place in the ring
+    int at = 0;                   // the step's place in the ring
     read(lds, 0, 0);
     for (int step = 0; step < steps; ++step) {
         const char* const now = lds + at * kBuffer;
