@@ -270,6 +270,22 @@ int escoin_linear_forward(const escoin_linear_desc *desc, const void *plan_host,
 /* host: up to how many tokens a call with this plan reads the kept weights only; or an error code */
 int escoin_linear_few_tokens(const escoin_linear_desc *desc, const void *plan_host);
 
+/* host: the kernel that a call with this descriptor and plan takes, for reports and tests.  All zeros for a call without tokens. */
+typedef struct escoin_linear_kernel_info {
+    int32_t kept;         /* 1: reads the kept weights; 0: the whole ones, tile by tile               */
+    int32_t rows, tokens; /* of weights and of activations, to a workgroup                            */
+    int32_t waves;
+    int32_t inputs;       /* 0: from any place, by way of registers; 1: 16 bytes a lane to registers; */
+                          /* 2: 16 bytes a lane copied to LDS                                         */
+    int32_t pieces;       /* kept: 16-byte pieces that a lane loads of a tile's values                */
+    int32_t lane_words;   /* kept: 32-bit words of LDS that are a lane's own                          */
+    int32_t steps;        /* whole: steps along the columns that LDS holds                            */
+    int32_t step_bytes;   /* whole: bytes of a row to a step                                          */
+    int32_t lds_bytes;    /* of a workgroup                                                           */
+} escoin_linear_kernel_info;
+/* d_in: where the call's input will lie (its alignment counts; nothing is read) */
+int escoin_linear_kernel(const escoin_linear_desc *desc, const void *plan_host, const void *d_in, escoin_linear_kernel_info *info);
+
 enum { ESCOIN_NORM_NONE = 0, ESCOIN_NORM_RMS = 1, ESCOIN_NORM_LAYER = 2 };
 
 typedef struct escoin_norm_desc {

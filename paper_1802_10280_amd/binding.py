@@ -34,6 +34,10 @@ class escoin_linear_desc(ctypes.Structure):
                 + [(k, ctypes.c_int64) for k in ("ld_in", "ld_out", "ld_residual")])
 
 
+class escoin_linear_kernel_info(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("kept", "rows", "tokens", "waves", "inputs", "pieces", "lane_words", "steps", "step_bytes", "lds_bytes")]
+
+
 class escoin_norm_desc(ctypes.Structure):
     _fields_ = ([(k, ctypes.c_int32) for k in ("T", "D", "type", "post", "pre", "gate_rows")]
                 + [(k, ctypes.c_float) for k in ("eps", "alpha", "beta", "weight_offset")]
@@ -83,6 +87,7 @@ def lib() -> ctypes.CDLL:
         L.escoin_linear_plan_build.argtypes = [LD, vp, vp, vp, vp, ctypes.c_size_t]
         L.escoin_linear_forward.argtypes = [LD, vp, vp, vp, vp, vp, vp, ctypes.c_uint32, vp]
         L.escoin_linear_few_tokens.argtypes = [LD, vp]
+        L.escoin_linear_kernel.argtypes = [LD, vp, vp, ctypes.POINTER(escoin_linear_kernel_info)]
         L.escoin_norm_check_desc.argtypes = [ND]
         L.escoin_norm_forward.argtypes = [ND, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         _lib = L
@@ -342,6 +347,13 @@ def escoin_linear_few_tokens(desc, plan_host: np.ndarray) -> int:
     if rc < 0:
         _check(rc, "escoin_linear_few_tokens")
     return rc
+
+
+def escoin_linear_kernel(desc, plan_host: np.ndarray, address: int = 0) -> dict:
+    """Which kernel a call takes whose input lies at `address` (0: wherever rows start on 16 bytes)."""
+    info = escoin_linear_kernel_info()
+    _check(lib().escoin_linear_kernel(ctypes.byref(desc), _plan_header(plan_host), address, ctypes.byref(info)), "escoin_linear_kernel")
+    return {k: int(getattr(info, k)) for k, _ in info._fields_}
 
 
 class _LinearHeader(ctypes.Structure):

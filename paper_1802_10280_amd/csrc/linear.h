@@ -66,7 +66,13 @@ struct LinearArgs {
     uint32_t flags;
 };
 
-int launch_linear_few(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, hipStream_t stream);
-int launch_linear_many(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, hipStream_t stream);
+// How a call goes out: on a stream, or, with `told`, not at all, and it is told which kernel it would be.
+struct LinearCall {
+    hipStream_t stream;
+    escoin_linear_kernel_info* told;
+};
+
+int launch_linear_few(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, const LinearCall& call);
+int launch_linear_many(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, const LinearCall& call);
 
 }  // namespace escoin

@@ -14,9 +14,10 @@ constexpr int few_waves(int type, int NT) { return NT > 1 || type == ESCOIN_T_F3
 // tokens are but a few, they are read together anyway.
 enum { kInElements, kInRegisters, kInLds };
 
-// LDS of a wave: a column of words for each lane (it reads up to two behind its last), and a tile's inputs.
-constexpr int few_columns(int chunks) { return (4 * chunks + 2) * 256; }
-constexpr int few_buffer(int type, int in, int NT, int chunks) { return few_columns(chunks) + (in == kInLds ? NT * (type == ESCOIN_T_F32 ? 8192 : 4096) : 0); }
+// LDS of a wave: a column of words for each lane, and a tile's inputs.  Where its last places are empty, a lane reads behind its last word
+// (and drops it): 16-bit values come by three words, fp32 ones by one.
+constexpr int few_columns(int type, int chunks) { return (4 * chunks + (type == ESCOIN_T_F32 ? 1 : 3)) * 256; }
+constexpr int few_buffer(int type, int in, int NT, int chunks) { return few_columns(type, chunks) + (in == kInLds ? NT * (type == ESCOIN_T_F32 ? 8192 : 4096) : 0); }
 
 // Exclusive sums over the lanes of a wave.
 __device__ inline int lanes_before(int n) {
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(64 * few_waves(TYPE, NT)) void linear_few_kernel(co
     extern __shared__ char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     constexpr int kSize = sizeof(typename Num<TYPE>::type), kParts = kSize == 4 ? 2 : 1, kBlockBytes = 32 * kSize;
-    constexpr int kColumns = few_columns(CHUNKS), kRowBytes = kTileCols * kSize, kX = IN == kInLds ? 4 * NT * kParts : 0;
+    constexpr int kColumns = few_columns(TYPE, CHUNKS), kRowBytes = kTileCols * kSize, kX = IN == kInLds ? 4 * NT * kParts : 0;
     constexpr int kBuffer = kColumns + kX * 1024;
     const int rt = blockIdx.x, token0 = blockIdx.y * NT * 16;
     const uint32_t picks = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds, column = picks + 128 + wave * kBuffer + lane * 4;
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(64 * few_waves(TYPE, NT)) void linear_few_kernel(co
 }
 
 template <int TYPE, bool GATED, int IN, int NT, int CHUNKS>
-int launch_one(const LinearArgs& a, hipStream_t stream) {
+int launch_one(const LinearArgs& a, const LinearCall& call) {
     const dim3 grid((unsigned)a.row_tiles, (unsigned)((a.T + NT * 16 - 1) / (NT * 16)));
     constexpr int waves_at_most = few_waves(TYPE, NT);
     int waves = waves_at_most;
@@ -248,52 +249,56 @@ int launch_one(const LinearArgs& a, hipStream_t stream) {
     waves = std::min(waves, a.col_tiles);
     const int lds = 128 + waves * kWave;
     if (!grid_fits((double)grid.x * grid.y, 64 * waves)) return ESCOIN_ERANGE;
+    if (call.told) {
+        *call.told = {1, kTileRows, NT * 16, waves, IN, CHUNKS, few_columns(TYPE, CHUNKS) / 256, 0, 0, lds};
+        return ESCOIN_OK;
+    }
     const auto kernel = linear_few_kernel<TYPE, GATED, IN, NT, CHUNKS>;
     const int rc = lds > 64 * 1024 ? allow_dynamic_lds((const void*)kernel, lds) : ESCOIN_OK;
-    return rc != ESCOIN_OK ? rc : launch(kernel, grid, dim3(64 * waves), (size_t)lds, stream, a);
+    return rc != ESCOIN_OK ? rc : launch(kernel, grid, dim3(64 * waves), (size_t)lds, call.stream, a);
 }
 
 template <int TYPE, bool GATED, int IN, int NT>
-int launch_chunks(const LinearHeader& h, const LinearArgs& a, hipStream_t stream) {
+int launch_chunks(const LinearHeader& h, const LinearArgs& a, const LinearCall& call) {
     const int chunks = (h.most_lane_words + 3) / 4;
     if constexpr (TYPE == ESCOIN_T_F32) {
-        if (chunks > 5) return launch_one<TYPE, GATED, IN, NT, 8>(a, stream);
-        if (chunks > 4) return launch_one<TYPE, GATED, IN, NT, 5>(a, stream);
+        if (chunks > 5) return launch_one<TYPE, GATED, IN, NT, 8>(a, call);
+        if (chunks > 4) return launch_one<TYPE, GATED, IN, NT, 5>(a, call);
     } else if (chunks > 4) {
-        return launch_one<TYPE, GATED, IN, NT, 5>(a, stream);
+        return launch_one<TYPE, GATED, IN, NT, 5>(a, call);
     }
-    if (chunks > 3) return launch_one<TYPE, GATED, IN, NT, 4>(a, stream);
-    if (chunks > 2) return launch_one<TYPE, GATED, IN, NT, 3>(a, stream);
-    if (chunks > 1) return launch_one<TYPE, GATED, IN, NT, 2>(a, stream);
-    return launch_one<TYPE, GATED, IN, NT, 1>(a, stream);
+    if (chunks > 3) return launch_one<TYPE, GATED, IN, NT, 4>(a, call);
+    if (chunks > 2) return launch_one<TYPE, GATED, IN, NT, 3>(a, call);
+    if (chunks > 1) return launch_one<TYPE, GATED, IN, NT, 2>(a, call);
+    return launch_one<TYPE, GATED, IN, NT, 1>(a, call);
 }
 
 template <int TYPE, bool GATED>
-int launch_tokens(const LinearHeader& h, const LinearArgs& a, bool wide, hipStream_t stream) {
+int launch_tokens(const LinearHeader& h, const LinearArgs& a, bool wide, const LinearCall& call) {
     // As many tokens to a workgroup as there are, up to 64: the weights are unfolded once for all of them (64 tokens, 12288 to 4096 at 50 %:
     // 33.8 us, by 32 40.3, by 16 47.2).  But where workgroups of 16 do not outnumber the compute units they are done sooner (1024 to 1024: 5.9, 6.7 by 32).
     const auto blocks = [&](int tokens) { return (int64_t)a.row_tiles * ((a.T + tokens - 1) / tokens); };
     const int nt = blocks(16) <= 256 ? 1 : a.T <= 32 || blocks(32) <= 256 ? 2 : 4;
-    if (!wide) return a.T <= 16 || nt == 1 ? launch_chunks<TYPE, GATED, kInElements, 1>(h, a, stream) : launch_chunks<TYPE, GATED, kInElements, 2>(h, a, stream);
-    if (a.T <= 4) return launch_chunks<TYPE, GATED, kInRegisters, 1>(h, a, stream);
-    if (a.T <= 16 || nt == 1) return launch_chunks<TYPE, GATED, kInLds, 1>(h, a, stream);
+    if (!wide) return a.T <= 16 || nt == 1 ? launch_chunks<TYPE, GATED, kInElements, 1>(h, a, call) : launch_chunks<TYPE, GATED, kInElements, 2>(h, a, call);
+    if (a.T <= 4) return launch_chunks<TYPE, GATED, kInRegisters, 1>(h, a, call);
+    if (a.T <= 16 || nt == 1) return launch_chunks<TYPE, GATED, kInLds, 1>(h, a, call);
     if constexpr (TYPE != ESCOIN_T_F32)  // (there are not the registers for more inputs)
-        if (nt == 4) return launch_chunks<TYPE, GATED, kInLds, 4>(h, a, stream);
-    return launch_chunks<TYPE, GATED, kInLds, 2>(h, a, stream);
+        if (nt == 4) return launch_chunks<TYPE, GATED, kInLds, 4>(h, a, call);
+    return launch_chunks<TYPE, GATED, kInLds, 2>(h, a, call);
 }
 
 template <int TYPE>
-int launch_type(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, hipStream_t stream) {
+int launch_type(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, const LinearCall& call) {
     const bool wide = wide_input(a, d.size());
-    return d.gated ? launch_tokens<TYPE, true>(h, a, wide, stream) : launch_tokens<TYPE, false>(h, a, wide, stream);
+    return d.gated ? launch_tokens<TYPE, true>(h, a, wide, call) : launch_tokens<TYPE, false>(h, a, wide, call);
 }
 
 }  // namespace
 
-int launch_linear_few(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, hipStream_t stream) {
-    if (d.type == ESCOIN_T_F32) return launch_type<ESCOIN_T_F32>(d, h, a, stream);
-    if (d.type == ESCOIN_T_F16) return launch_type<ESCOIN_T_F16>(d, h, a, stream);
-    return launch_type<ESCOIN_T_BF16>(d, h, a, stream);
+int launch_linear_few(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, const LinearCall& call) {
+    if (d.type == ESCOIN_T_F32) return launch_type<ESCOIN_T_F32>(d, h, a, call);
+    if (d.type == ESCOIN_T_F16) return launch_type<ESCOIN_T_F16>(d, h, a, call);
+    return launch_type<ESCOIN_T_BF16>(d, h, a, call);
 }
 
 }  // namespace escoin

@@ -190,13 +190,17 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
 }
 
 template <int TYPE, bool GATED, bool WIDE, int BM, int BN, int WM, int WN, int WK, int NS, int SF = kStepFrags>
-int launch_one(const LinearArgs& a, hipStream_t stream) {
+int launch_one(const LinearArgs& a, const LinearCall& call) {
     constexpr int kLds = std::max(NS * (BM + BN) * SF * 32, WM * WN * WK * 32 * many_pitch(BM / 32 / WM)), kThreads = 64 * WM * WN * WK;
     const int64_t rows = (a.rows + BM - 1) / BM, tokens = ((int64_t)a.T + BN - 1) / BN;
     if (!grid_fits((double)rows * tokens, kThreads)) return ESCOIN_ERANGE;
+    if (call.told) {
+        *call.told = {0, BM, BN, kThreads / 64, WIDE ? 2 : 0, 0, 0, NS, SF * 32, kLds};
+        return ESCOIN_OK;
+    }
     const auto kernel = linear_many_kernel<TYPE, GATED, WIDE, BM, BN, WM, WN, WK, NS, SF>;
     const int rc = kLds > 64 * 1024 ? allow_dynamic_lds((const void*)kernel, kLds) : ESCOIN_OK;
-    return rc != ESCOIN_OK ? rc : launch(kernel, dim3((unsigned)(rows * tokens)), dim3(kThreads), (size_t)kLds, stream, a, (int)rows, (int)tokens);
+    return rc != ESCOIN_OK ? rc : launch(kernel, dim3((unsigned)(rows * tokens)), dim3(kThreads), (size_t)kLds, call.stream, a, (int)rows, (int)tokens);
 }
 
 // Which tile: the one whose steps take the least time, by how many of its tiles the fullest compute unit gets.  Microseconds a step of 128 bytes a row,
@@ -204,7 +208,7 @@ int launch_one(const LinearArgs& a, hipStream_t stream) {
 // brings 16 KB for 0.5 MFLOP, of 256 by 256 64 KB for 8), fp32 by the matrix cores with any, so that there the smallest come
 // first.  Inputs that come through registers have the tiles whose ring holds three steps or more.
 template <int TYPE, bool GATED, bool WIDE>
-int launch_tile(const LinearArgs& a, hipStream_t stream) {
+int launch_tile(const LinearArgs& a, const LinearCall& call) {
     const auto tiles = [&](int rows, int tokens) { return ((int64_t)a.rows + rows - 1) / rows * (((int64_t)a.T + tokens - 1) / tokens); };
     const auto rounds = [](int64_t n, int units) { return (double)((n + units - 1) / units); };
     if constexpr (TYPE == ESCOIN_T_F32) {
@@ -212,9 +216,9 @@ int launch_tile(const LinearArgs& a, hipStream_t stream) {
         const double t32 = n32 <= 256 ? 0.24 : 0.255 * rounds(n32, 256), t64 = 0.52 * rounds(tiles(64, 64), 256), t128 = 1.95 * rounds(tiles(128, 128), 256);
         // (two small tiles to a compute unit or fewer: twice the columns to a step, by more waves; 1001 to 1503, 250 tokens 16.7 us and 18.4)
         if (t32 < std::min(t64, t128))
-            return n32 <= 512 ? launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 4, 3, 8>(a, stream) : launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, stream);
-        if (t64 < t128) return launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, stream);
-        return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, WIDE ? 2 : 4>(a, stream);
+            return n32 <= 512 ? launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 4, 3, 8>(a, call) : launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, call);
+        if (t64 < t128) return launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, call);
+        return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, WIDE ? 2 : 4>(a, call);
     } else {
         // one tile of 128 by 128 to a compute unit, four steps on their way; or two, a step each
         const int64_t n128 = tiles(128, 128);
@@ -223,33 +227,33 @@ int launch_tile(const LinearArgs& a, hipStream_t stream) {
         const double t128 = n128 <= 256 ? 0.46 : WIDE ? 1.05 * rounds(n128, 512) : 0.46 * rounds(n128, 256);
         if constexpr (WIDE) {
             const double tall = 0.97 * rounds(tiles(256, 128), 256), large = 1.6 * rounds(tiles(256, 256), 256);
-            if (large < std::min(std::min(small, t128), tall)) return launch_one<TYPE, GATED, WIDE, 256, 256, 2, 4, 1, 2>(a, stream);
-            if (tall < std::min(small, t128)) return launch_one<TYPE, GATED, WIDE, 256, 128, 2, 2, 2, 3>(a, stream);
+            if (large < std::min(std::min(small, t128), tall)) return launch_one<TYPE, GATED, WIDE, 256, 256, 2, 4, 1, 2>(a, call);
+            if (tall < std::min(small, t128)) return launch_one<TYPE, GATED, WIDE, 256, 128, 2, 2, 2, 3>(a, call);
         }
         // (one small tile to a compute unit: half as many steps of twice the columns, by more waves; 2560 to 2560, 53 tokens 9.4 us and 10.3)
         if (t32 < std::min(t64, t128))
-            return n32 <= 256 ? launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 4, 3, 8>(a, stream) : launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, stream);
+            return n32 <= 256 ? launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 4, 3, 8>(a, call) : launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, call);
         if (t64 < t128)
-            return n64 <= 256 ? launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3, 8>(a, stream) : launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, stream);
+            return n64 <= 256 ? launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3, 8>(a, call) : launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, call);
         if constexpr (WIDE)
-            if (n128 > 256) return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, 2>(a, stream);
-        return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, 4>(a, stream);
+            if (n128 > 256) return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, 2>(a, call);
+        return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, 4>(a, call);
     }
 }
 
 template <int TYPE>
-int launch_type(const LinearDims& d, const LinearArgs& a, hipStream_t stream) {
+int launch_type(const LinearDims& d, const LinearArgs& a, const LinearCall& call) {
     const bool wide = wide_input(a, d.size());
-    if (d.gated) return wide ? launch_tile<TYPE, true, true>(a, stream) : launch_tile<TYPE, true, false>(a, stream);
-    return wide ? launch_tile<TYPE, false, true>(a, stream) : launch_tile<TYPE, false, false>(a, stream);
+    if (d.gated) return wide ? launch_tile<TYPE, true, true>(a, call) : launch_tile<TYPE, true, false>(a, call);
+    return wide ? launch_tile<TYPE, false, true>(a, call) : launch_tile<TYPE, false, false>(a, call);
 }
 
 }  // namespace
 
-int launch_linear_many(const LinearDims& d, const LinearHeader&, const LinearArgs& a, hipStream_t stream) {
-    if (d.type == ESCOIN_T_F32) return launch_type<ESCOIN_T_F32>(d, a, stream);
-    if (d.type == ESCOIN_T_F16) return launch_type<ESCOIN_T_F16>(d, a, stream);
-    return launch_type<ESCOIN_T_BF16>(d, a, stream);
+int launch_linear_many(const LinearDims& d, const LinearHeader&, const LinearArgs& a, const LinearCall& call) {
+    if (d.type == ESCOIN_T_F32) return launch_type<ESCOIN_T_F32>(d, a, call);
+    if (d.type == ESCOIN_T_F16) return launch_type<ESCOIN_T_F16>(d, a, call);
+    return launch_type<ESCOIN_T_BF16>(d, a, call);
 }
 
 }  // namespace escoin

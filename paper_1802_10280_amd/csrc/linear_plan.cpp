@@ -225,6 +225,21 @@ int make_linear_dims(const escoin_linear_desc* desc, LinearDims* d) {
     return ESCOIN_OK;
 }
 
+// What a call's kernel goes by: sizes, pitches in bytes and where the input lies.
+static LinearArgs linear_sizes(const LinearDims& d, const void* d_in) {
+    LinearArgs a = {};
+    const int size = d.size();
+    a.in = (const char*)d_in;
+    a.T = d.T; a.K = d.K; a.M = d.M; a.rows = d.rows();
+    a.row_tiles = d.row_tiles(); a.col_tiles = d.col_tiles(); a.row_frags = d.row_frags(); a.col_frags = d.col_frags();
+    a.ld_in = d.ld_in * size; a.ld_out = d.ld_out * size; a.ld_residual = d.ld_residual * size;
+    return a;
+}
+
+static int linear_launch(const LinearDims& d, const LinearHeader& h, const LinearArgs& a, const LinearCall& call) {
+    return d.T <= h.few_tokens ? launch_linear_few(d, h, a, call) : launch_linear_many(d, h, a, call);
+}
+
 int linear_header(const LinearDims& d, const void* plan, LinearHeader* h) {
     if (!plan) return ESCOIN_EINVAL;
     memcpy(h, plan, sizeof(*h));
@@ -298,9 +313,8 @@ int escoin_linear_forward(const escoin_linear_desc* desc, const void* plan_host,
     if (((uintptr_t)d_plan & 15) || (((uintptr_t)d_in | (uintptr_t)d_out) & (size - 1)) || ((flags & ESCOIN_F_BIAS) && ((uintptr_t)d_bias & (size - 1))) ||
         ((flags & ESCOIN_F_RESIDUAL) && ((uintptr_t)d_residual & (size - 1))))
         return ESCOIN_EINVAL;
-    LinearArgs a;
+    LinearArgs a = linear_sizes(d, d_in);
     const char* const p = (const char*)d_plan;
-    a.in = (const char*)d_in;
     a.out = (char*)d_out;
     a.bias = flags & ESCOIN_F_BIAS ? (const char*)d_bias : nullptr;
     a.residual = flags & ESCOIN_F_RESIDUAL ? (const char*)d_residual : nullptr;
@@ -309,11 +323,19 @@ int escoin_linear_forward(const escoin_linear_desc* desc, const void* plan_host,
     a.start = (const uint32_t*)(p + h.off_start);
     a.kept = p + h.off_kept;
     a.whole = p + h.off_whole;
-    a.T = d.T; a.K = d.K; a.M = d.M; a.rows = d.rows();
-    a.row_tiles = d.row_tiles(); a.col_tiles = d.col_tiles(); a.row_frags = d.row_frags(); a.col_frags = d.col_frags();
-    a.ld_in = d.ld_in * size; a.ld_out = d.ld_out * size; a.ld_residual = d.ld_residual * size;
     a.flags = flags;
-    return d.T <= h.few_tokens ? launch_linear_few(d, h, a, (hipStream_t)hip_stream) : launch_linear_many(d, h, a, (hipStream_t)hip_stream);
+    return linear_launch(d, h, a, {(hipStream_t)hip_stream, nullptr});
+}
+
+int escoin_linear_kernel(const escoin_linear_desc* desc, const void* plan_host, const void* d_in, escoin_linear_kernel_info* info) {
+    LinearDims d;
+    LinearHeader h;
+    int rc = make_linear_dims(desc, &d);
+    if (rc == ESCOIN_OK) rc = linear_header(d, plan_host, &h);
+    if (rc != ESCOIN_OK) return rc;
+    if (!info || ((uintptr_t)d_in & (d.size() - 1))) return ESCOIN_EINVAL;
+    *info = {};
+    return d.T == 0 ? ESCOIN_OK : linear_launch(d, h, linear_sizes(d, d_in), {nullptr, info});
 }
 
 }  // extern "C"
