@@ -364,6 +364,7 @@ class _LinearHeader(ctypes.Structure):
 
 
 _BYTES, _HEADER_BYTES = np.dtype(np.uint8), ctypes.sizeof(_LinearHeader)
+_TOTAL = slice(_LinearHeader.total_bytes.offset, _HEADER_BYTES)  # where it says how long a plan is
 
 
 def _plan_header(plan: np.ndarray) -> bytes:
@@ -385,7 +386,7 @@ def escoin_linear_forward(desc, plan_host: np.ndarray, d_plan, d_in, d_out, d_bi
     args = (t.rows(d_in, T, desc.K, desc.ld_in), t.rows(d_out, T, desc.M, desc.ld_out), t.vector(d_bias, rows),
             t.rows(d_residual, T, desc.M, desc.ld_residual))
     plan = _plan_header(plan_host)
-    if d_plan.get_device() != t.device or d_plan.nbytes < plan_host.size or not d_plan.is_contiguous():
+    if d_plan is None or d_plan.get_device() != t.device or d_plan.nbytes < int.from_bytes(plan[_TOTAL], "little") or not d_plan.is_contiguous():
         raise TypeError("the plan's copy has to be whole and on the tensors' device")
     t.call("escoin_linear_forward", lib().escoin_linear_forward, ctypes.byref(desc), plan, d_plan.data_ptr(), *args, flags, stream=stream)
 

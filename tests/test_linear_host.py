@@ -306,3 +306,25 @@ def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
             for b in bad:
                 with pytest.raises(TypeError):
                     esc.escoin_norm_forward(d, **{**ok, name: b})
+
+
+def test_a_plans_copy_is_as_long_as_its_header_says(monkeypatch):
+    """The host's part may be the header alone; the device's copy is what kernels read, and has to be whole all the same."""
+    from paper_1802_10280_amd import binding
+
+    def call(self, where, fn, *args, stream):
+        raise Reached
+
+    monkeypatch.setattr(binding._Rows, "call", call)
+    T, K, M = 4, 640, 48
+    d = esc.make_linear_desc(T, K, M, esc.T_BF16)
+    plan = esc.escoin_linear_plan_build(d, *ff.pruned(M, K, 0.5, 1, 2)[1])
+    x, out = Tensor([T, K]), Tensor([T, M])
+    for host in (plan, plan[:256], np.concatenate([plan, plan[:64]])):
+        with pytest.raises(Reached):
+            esc.escoin_linear_forward(d, host, Tensor([plan.nbytes // 2]), x, out)
+        for short in (128, plan.nbytes // 2 - 1):
+            with pytest.raises(TypeError):
+                esc.escoin_linear_forward(d, host, Tensor([short]), x, out)
+    with pytest.raises(TypeError):
+        esc.escoin_linear_forward(d, plan, None, x, out)
