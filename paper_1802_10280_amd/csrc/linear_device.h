@@ -74,20 +74,50 @@ __device__ inline f16v mfma32(u4 w, u4 x, f16v c) {
 
 // z / (1 + exp(-u)).  For outputs of 16 bits the instructions' own exponential and reciprocal, each a step of fp32 or two off, do; the
 // library's forms, some 40 instructions, are an eighth of a long prompt's time.
-template <int TYPE>
-__device__ inline float logistic(float z, float u) {
-    if constexpr (TYPE == ESCOIN_T_F32) return z / (1.0f + expf(-u));
-    else return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * u));
+// Far below zero it is z exp(u), to all of fp32's bits, in two factors that stay in range: exp(-u) passes 2^128, and from 2^126 on the reciprocal
+// instruction gives zero, while the result is a number of fp32 and bf16 still.
+template <int TYPE, int N>
+__device__ inline void logistic(float (&z)[N], const float (&u)[N]) {
+    if constexpr (TYPE == ESCOIN_T_F32) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool far = u[i] < -80.0f;
+            const float e = expf(far ? 0.5f * u[i] : -u[i]);
+            z[i] = far ? z[i] * e * e : z[i] / (1.0f + e);
+        }
+    } else {
+        float p[N];
+        bool far = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) p[i] = -1.44269504088896341f * u[i], far |= p[i] > 120.0f;
+        if (__builtin_expect(far, 0)) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float e = __builtin_amdgcn_exp2f(p[i] > 120.0f ? 64.0f - p[i] : p[i]);
+                z[i] = p[i] > 120.0f ? z[i] * e * 0x1p-64f : z[i] * __builtin_amdgcn_rcpf(1.0f + e);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] *= __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(p[i]));
+    }
 }
 
-template <int TYPE>
-__device__ inline float activate(float z, uint32_t flags) {
-    if (flags & ESCOIN_F_RELU) return z > 0.0f ? z : 0.0f;
-    if (flags & ESCOIN_F_SILU) return logistic<TYPE>(z, z);
-    if (flags & ESCOIN_F_GELU) return 0.5f * z * erfcf(-0.70710678118654752f * z);
-    // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), which keeps its bits where tanh is near -1
-    if (flags & ESCOIN_F_GELU_TANH) return logistic<TYPE>(z, 1.5957691216057308f * (z + 0.044715f * z * z * z));
-    return z;
+template <int TYPE, int N>
+__device__ inline void activate(float (&z)[N], uint32_t flags) {
+    if (flags & ESCOIN_F_RELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = z[i] > 0.0f ? z[i] : 0.0f;
+    } else if (flags & ESCOIN_F_GELU) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) z[i] = 0.5f * z[i] * erfcf(-0.70710678118654752f * z[i]);
+    } else if (flags & (ESCOIN_F_SILU | ESCOIN_F_GELU_TANH)) {
+        // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), which keeps its bits where tanh is near -1
+        float u[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = flags & ESCOIN_F_SILU ? z[i] : 1.5957691216057308f * (z[i] + 0.044715f * z[i] * z[i] * z[i]);
+        logistic<TYPE>(z, u);
+    }
 }
 
 // What follows the sums of R * 4 neighbouring rows (from `row`, a multiple of R * 4) for one token: bias, activation, gate,
@@ -116,16 +146,20 @@ __device__ inline void finish(const LinearArgs& a, const f4 (&z)[R], int row, in
     if constexpr (GATED) {
         N c[kOut];
         if (a.bias) get(a.bias + m0 * sizeof(N), b), get(a.bias + ((int64_t)a.M + m0) * sizeof(N), c);
+        float u[kOut];
 #pragma unroll
         for (int i = 0; i < kOut; ++i) {
-            float g = z[i / 2][i % 2 * 2], u = z[i / 2][i % 2 * 2 + 1];
-            if (a.bias) g += (float)b[i], u += (float)c[i];
-            v[i] = activate<TYPE>(g, a.flags) * u;
+            v[i] = z[i / 2][i % 2 * 2], u[i] = z[i / 2][i % 2 * 2 + 1];
+            if (a.bias) v[i] += (float)b[i], u[i] += (float)c[i];
         }
+        activate<TYPE>(v, a.flags);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) v[i] *= u[i];
     } else {
         if (a.bias) get(a.bias + m0 * sizeof(N), b);
 #pragma unroll
-        for (int i = 0; i < kOut; ++i) v[i] = activate<TYPE>(a.bias ? z[i / 4][i % 4] + (float)b[i] : z[i / 4][i % 4], a.flags);
+        for (int i = 0; i < kOut; ++i) v[i] = a.bias ? z[i / 4][i % 4] + (float)b[i] : z[i / 4][i % 4];
+        activate<TYPE>(v, a.flags);
     }
     if (a.residual) {
         get(a.residual + token * a.ld_residual + m0 * sizeof(N), b);

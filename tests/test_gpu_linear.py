@@ -315,3 +315,25 @@ def test_kept_weights_for_many_tokens(type, K, M, T, gated):
     layer = Layer(K, M, type, gated, sparsity=0.9)
     assert layer.few >= T
     layer.check(T, BIAS | RESIDUAL | GELU_TANH)
+
+
+@gpu
+@TYPES
+@pytest.mark.parametrize("act", [SILU, GELU_TANH])
+@pytest.mark.parametrize("T", [3, 300])
+def test_activations_far_below_zero(type, act, T):
+    """z / (1 + exp(-u)) as long as the type holds it, where exp(-u) is beyond fp32.  Relative to the value: u is off by six half steps of
+    itself (SiLU: by none), its product with log2 e and that one's distance from 64 by three more, each worth |u| of the value; an
+    exponential and three products by eight."""
+    K = 64
+    layer = Layer(K, K, type)
+    layer.w = np.eye(K)
+    layer.plan = esc.escoin_linear_plan_build(esc.make_linear_desc(1000, K, K, type), *ff.to_csr(layer.w))
+    import torch
+    layer.d_plan = torch.from_numpy(layer.plan).cuda()
+    z = ff.rounded(np.linspace(-110.0 if act == SILU else -11.0, 4.0, T * K).reshape(T, K), type)
+    got = layer.forward(ff.to_dev(z, type), act).double().cpu().numpy()
+    u = z if act == SILU else 2 * np.sqrt(2 / np.pi) * (z + 0.044715 * z ** 3)
+    ref = z / (1 + np.exp(-u))
+    off = np.abs(ref) * ((9 if act == GELU_TANH else 3) * np.abs(u) + 8) * ff.F32
+    ff.within(got, ref, off + ff.HALF[type] * (np.abs(ref) + off) + ff.TINY[type])
