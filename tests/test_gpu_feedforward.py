@@ -97,3 +97,18 @@ def test_bundled_blocks():
         r = FeedForwardRunner(wl.make_block(name))
         r.run()
         check(r)
+
+
+def test_the_bundled_prompt():
+    """The bundled block whose products go through the tiled kernel: tokens about every tile's edges and some others, all their outputs."""
+    from types import SimpleNamespace
+    from paper_1802_10280_amd.runner import FeedForwardRunner
+    r = FeedForwardRunner(wl.make_block(wl.CONFIG_BLOCKS["feedforward"][2]))
+    T = r.block.spec.T
+    for desc, plan, d_in in ((r.up_desc, r.up_plan, r.d_n), (r.down_desc, r.down_plan, r.d_g)):
+        assert not esc.escoin_linear_kernel(desc, plan, d_in.data_ptr())["kept"]
+    r.run()
+    assert all(t.isfinite().all() for t in (r.d_n, r.d_g, r.d_d, r.d_h, r.d_next))
+    edges = [t for e in range(0, T, 128) for t in (e, e + 31, e + 127)]
+    rows = sorted({*edges, *np.random.default_rng(8).integers(0, T, 48).tolist()})
+    check(SimpleNamespace(block=r.block, before=None, **{k: getattr(r, k)[rows] for k in ("d_x", "d_n", "d_g", "d_d", "d_h", "d_next")}))
