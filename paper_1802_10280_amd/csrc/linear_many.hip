@@ -35,8 +35,8 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
     place(n_row_tiles, n_token_tiles, &row_tile, &token_tile);
     const int row0 = row_tile * BM, token0 = token_tile * BN, end = a.K * kSize, steps = (a.col_frags + SF - 1) / SF;
 
-    // What a thread copies: of the weights 16 bytes of the wave's share of the fragments, of the inputs a piece of every kThreads / 8
-    // tokens, by way of buffers: 32-bit offsets leave the registers to the sums, and the compiler waits for every LDS read
+    // What a thread copies: of the weights 16 bytes of the wave's share of the fragments, of the inputs a piece of every
+    // kThreads / kTokenPieces tokens, by way of buffers: 32-bit offsets leave the registers to the sums, and the compiler waits for every LDS read
     // as long as a copy to LDS by a global address is on its way.
     const auto turned = [](int token) { return SF == 4 ? token >> 1 & 7 : token & 15; };
     const int my_token = tid / kTokenPieces, piece = tid % kTokenPieces ^ turned(my_token);
@@ -118,6 +118,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
         }
     arrived(steps < NS);
     constexpr int kOwn = SF / WK;  // fragments of a step that are a wave's
+    static_assert(kOwn % 2 == 0, "a step's first fragments take the registers that its last ones leave alone");
     int at = 0;                   // the step's place in the ring
     read(lds, 0, 0);
     for (int step = 0; step < steps; ++step) {
@@ -137,13 +138,11 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void linear_many_kernel(const Li
         }
         if (step + 1 < steps) {
             arrived(!more);
-            if constexpr (kOwn > 1) read(lds + at * kBuffer, 0, 0);
+            read(lds + at * kBuffer, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
-        multiply((kOwn - 1) & 1, step * SF + (kOwn - 1) * WK + wk);
+        multiply(1, step * SF + (kOwn - 1) * WK + wk);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (kOwn == 1)
-            if (step + 1 < steps) read(lds + at * kBuffer, 0, 0);
     }
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
@@ -206,18 +205,17 @@ int launch_one(const LinearArgs& a, const LinearCall& call) {
 // Which tile: the one whose steps take the least time, by how many of its tiles the fullest compute unit gets.  Microseconds a step of 128 bytes a row,
 // measured with 256 to 25000 rows and 64 to 4096 tokens: 16-bit types are bound by the copies to LDS with small tiles (a step of 64 by 64
 // brings 16 KB for 0.5 MFLOP, of 256 by 256 64 KB for 8), fp32 by the matrix cores with any, so that there the smallest come
-// first.  Inputs that come through registers have the tiles whose ring holds three steps or more.
+// first (64 by 64 take 0.52, never less than the two of 64 by 32 in their place).  Inputs that come through registers have the tiles whose ring holds three steps or more.
 template <int TYPE, bool GATED, bool WIDE>
 int launch_tile(const LinearArgs& a, const LinearCall& call) {
     const auto tiles = [&](int rows, int tokens) { return ((int64_t)a.rows + rows - 1) / rows * (((int64_t)a.T + tokens - 1) / tokens); };
     const auto rounds = [](int64_t n, int units) { return (double)((n + units - 1) / units); };
     if constexpr (TYPE == ESCOIN_T_F32) {
         const int64_t n32 = tiles(64, 32);
-        const double t32 = n32 <= 256 ? 0.24 : 0.255 * rounds(n32, 256), t64 = 0.52 * rounds(tiles(64, 64), 256), t128 = 1.95 * rounds(tiles(128, 128), 256);
+        const double t32 = n32 <= 256 ? 0.24 : 0.255 * rounds(n32, 256), t128 = 1.95 * rounds(tiles(128, 128), 256);
         // (two small tiles to a compute unit or fewer: twice the columns to a step, by more waves; 1001 to 1503, 250 tokens 16.7 us and 18.4)
-        if (t32 < std::min(t64, t128))
+        if (t32 < t128)
             return n32 <= 512 ? launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 4, 3, 8>(a, call) : launch_one<TYPE, GATED, WIDE, 64, 32, 2, 1, 2, 4>(a, call);
-        if (t64 < t128) return launch_one<TYPE, GATED, WIDE, 64, 64, 2, 2, 2, 3>(a, call);
         return launch_one<TYPE, GATED, WIDE, 128, 128, 2, 2, 2, WIDE ? 2 : 4>(a, call);
     } else {
         // one tile of 128 by 128 to a compute unit, four steps on their way; or two, a step each

@@ -1,11 +1,15 @@
 """Which kernel a linear layer's call takes, as the library tells it, and that what such a kernel reads of its LDS is its own."""
 import ctypes
+import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
 
 import paper_1802_10280_amd as esc
 import feedforward as ff
+import linear_cases as lc
 
 
 def words_read(plan, rows, K, type):
@@ -80,3 +84,41 @@ def test_kernel_refusals():
                dict(desc=esc.make_linear_desc(-1, 6, 2, esc.T_F32))):
         assert call(**kw) == esc.EINVAL, kw
     assert not any(esc.escoin_linear_kernel(esc.make_linear_desc(0, 6, 2, esc.T_F32), plan).values())
+
+
+def compiled_kernels():
+    """The names of the linear layers' kernels in the built library: waves multiplied out."""
+    nm = shutil.which("nm")
+    if nm is None:
+        pytest.skip("no nm here")
+    text = subprocess.run([nm, "-C", esc.binding.LIB_PATH], check=True, capture_output=True, text=True, timeout=120).stdout
+    names = set(re.findall(r" (linear_(?:few|many)_kernel<[^>]*>)", text.replace("::", " ")))
+    out = set()
+    for n in names:
+        if n.startswith("linear_many"):
+            a = n[len("linear_many_kernel<"):-1].split(", ")
+            n = f"linear_many_kernel<{', '.join(a[:5])}, {int(a[5]) * int(a[6]) * int(a[7])} waves, {a[8]}, {a[9]}>"
+        out.add(n)
+    assert len(out) == len(names)
+    return out
+
+
+def test_every_kernel_in_the_library_is_one_that_a_tested_call_takes():
+    reached = set()
+    for size, types in lc.TYPES.items():
+        for type in types:
+            for gated in (False, True):
+                for case in [*lc.MANY, *lc.FEW]:
+                    if case[0] != size:
+                        continue
+                    _, place, K, rows, T, kernel = case
+                    d = esc.make_linear_desc(0, K, rows // 2 if gated else rows, type, gated)
+                    empty = esc.escoin_linear_plan_build(d, np.zeros(rows + 1, np.int32), np.zeros(0, np.int32), np.zeros(0, np.float32))
+                    for pieces in lc.PIECES[size] if case in lc.FEW else (1,):
+                        k = lc.kernel_of(d, lc.header_with(empty, most_tokens=1 << 20, most_lane_words=4 * pieces), T, place)
+                        if case in lc.FEW:
+                            assert (k["kept"], k["inputs"], k["tokens"], k["pieces"]) == (1, *kernel, pieces), (case, k)
+                        else:
+                            assert (k["kept"], k["rows"], k["tokens"], k["steps"], k["step_bytes"]) == (0, *kernel), (case, k)
+                        reached.add(lc.named(k, type, gated))
+    assert reached == compiled_kernels()
