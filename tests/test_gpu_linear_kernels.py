@@ -78,3 +78,29 @@ def test_kernels_for_few_tokens(place, K, rows, T, kernel, type, gated):
     for pieces, sparsity in lc.PIECES[4 if type == 0 else 2].items():
         k = run(type, gated, place, K, rows, T, sparsity, K + rows + pieces)
         assert (k["kept"], k["inputs"], k["tokens"], k["pieces"]) == (1, *kernel, pieces)
+
+
+@pytest.mark.parametrize("K,M,T,kept", [(1032, 2124, 29, 1), (1032, 300, 13, 1), (2328, 522, 240, 1), (256, 4096, 1000, 0), (256, 8192, 2048, 0)])
+def test_graphs_of_kernels_with_more_than_64_kb_of_lds(K, M, T, kept):
+    import torch
+    _, csr = ff.pruned(M, K, 0.3, K + T, 2)
+    plan = esc.escoin_linear_plan_build(esc.make_linear_desc(1 << 20, K, M, esc.T_BF16), *csr)
+    d_plan = torch.from_numpy(plan).cuda()
+    d = esc.make_linear_desc(T, K, M, esc.T_BF16)
+    x = torch.randn(T, K, device="cuda").bfloat16()
+    out = torch.empty(T, M, dtype=torch.bfloat16, device="cuda")
+    told = esc.escoin_linear_kernel(d, plan, x.data_ptr())
+    assert told["kept"] == kept and told["lds_bytes"] > 64 * 1024
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        esc.escoin_linear_forward(d, plan, d_plan, x, out, flags=SILU)
+    eager = torch.empty_like(out)
+    for k in range(3):
+        out.fill_(-1.0)
+        eager.fill_(1.0)
+        esc.escoin_linear_forward(d, plan, d_plan, x, eager, flags=SILU)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (out == eager).all() and eager.isfinite().all()
+        x.mul_(0.5)
