@@ -264,6 +264,8 @@ class _Rows:
         if not _torch_types:
             import torch
             _torch_types.extend((torch.float32, torch.float16, torch.bfloat16))
+        if not T_F32 <= type <= T_BF16:
+            raise EscoinError(EINVAL, f"unknown type {type}")
         self.type, self.device = _torch_types[type], -2    # (a CPU tensor's is -1)
 
     def _seen(self, t):

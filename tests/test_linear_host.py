@@ -328,3 +328,14 @@ def test_a_plans_copy_is_as_long_as_its_header_says(monkeypatch):
                 esc.escoin_linear_forward(d, host, Tensor([short]), x, out)
     with pytest.raises(TypeError):
         esc.escoin_linear_forward(d, plan, None, x, out)
+
+
+@pytest.mark.parametrize("type", [-1, 3, 99])
+def test_the_binding_refuses_unknown_types_as_the_library_does(type):
+    _, csr = ff.pruned(16, 64, 0.5, 1, 2)
+    plan = esc.escoin_linear_plan_build(esc.make_linear_desc(4, 64, 16, esc.T_BF16), *csr)
+    for call in (lambda: esc.escoin_linear_forward(esc.make_linear_desc(4, 64, 16, type), plan, Tensor([plan.nbytes // 2]), Tensor([4, 64]), Tensor([4, 16])),
+                 lambda: esc.escoin_norm_forward(esc.make_norm_desc(4, 64, type), Tensor([4, 64]), None, Tensor([4, 64]))):
+        with pytest.raises(esc.EscoinError) as e:
+            call()
+        assert e.value.code == esc.EINVAL
