@@ -309,7 +309,8 @@ int escoin_norm_check_desc(const escoin_norm_desc *desc);
  * n is the norm of h before h is rounded.
  *   d_x                  device, T x D
  *   d_y, d_gate          device; d_y NULL: h = alpha * x (post must be NONE then, and d_gate NULL); d_gate NULL: 1
- *   d_post_*, d_pre_*    device, D elements each; NULL: weight 1, bias 0; NULL for a norm that is NONE
+ *   d_post_*, d_pre_*    device, D elements each; a weight NULL: no factor (weight_offset is then unused), a bias NULL: none; NULL for a
+ *                        norm that is NONE
  *   d_h, d_n             device, T x D each; either may be NULL.  Each may be d_x or d_y itself with the same pitch; h and n
  *                        must not be the same.
  */

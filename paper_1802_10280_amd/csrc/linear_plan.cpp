@@ -43,7 +43,8 @@ inline uint16_t fp16_bits(float f) {
 // Up to how many tokens the kept weights are read.  Every workgroup unfolds them for itself, for 64 tokens at a time (fp32: 32): microseconds
 // a tile and compute unit, and two more to begin with than the tiled kernel where it is more than 32; inputs whose rows cannot all start on 16 bytes
 // cost more.  The tiled kernel's time is its steps (linear_many.hip), but no less than the whole weights take from memory; it
-// needs rows enough to be spread over the compute units.  Measured with 64 tokens at 50 %, kept against whole: 12288 to 4096 34
+// needs rows enough to be spread over the compute units.  All of it at 50 %: layers with fewer nonzeros, whose kept weights cost less, go by
+// the same numbers, and so by the tiled kernel somewhat early.  Measured with 64 tokens, kept against whole: 12288 to 4096 34
 // and 33 us, 12288 to 2048 21 and 32, 2560 to 2560 10.7 and 9.4, 4096 to 24576 73 and 34, at 32 tokens 37.7 and 32.1 (41 from memory).
 int few_tokens(const LinearDims& d) {
     const bool f32 = d.type == ESCOIN_T_F32;

@@ -90,7 +90,8 @@ TYPES = {"f32": B.T_F32, "f16": B.T_F16, "bf16": B.T_BF16}
 
 class FeedForwardRunner:
     """One pruned feed-forward block: n = norm(x); g = silu(n Wg) * (n Wu); d = g Wd; h = x + gate * norm(d); and the next
-    block's n = norm(h)."""
+    block's n = norm(h).  It owns the buffers of one number of tokens, and its plans; a program that has calls of several lengths makes
+    one plan for the longest, and calls the library with the length of each."""
 
     def __init__(self, block, stream=None, before=None, eps: float = 1e-5):
         """before: the runner of the block before this one, whose h and n this one reads (they need no norm of their own)."""
